@@ -40,7 +40,8 @@ typedef enum {
     Q8_ERR_ALIGN = 3,  /* a pointer breaks the alignment its type needs (4 bytes for float/int32) */
     Q8_ERR_FLAGS = 4,  /* unknown epilogue bit, or a flag without the pointer it needs */
     Q8_ERR_LAUNCH = 5,    /* the HIP runtime refused a launch */
-    Q8_ERR_TOO_LARGE = 6  /* q8_linear_f32_static: M*K exceeds Q8_STATIC_MAX_CODES */
+    Q8_ERR_TOO_LARGE = 6, /* q8_linear_f32_static: M*K exceeds Q8_STATIC_MAX_CODES */
+    Q8_ERR_OVERLAP = 7    /* 4-bit, grouped and routing entry points: an output shares memory with an input or another output */
 } q8_status;
 
 /* Largest reduction length: 128*128*K must stay below 2^31 so that no int8 input,
@@ -363,6 +364,118 @@ q8_status q8_embedding_sum3_layernorm(const int8_t* word, int64_t Vw, const int8
 q8_status q8_attention(const float* qkv, int64_t B, int64_t S, int heads, int d,
                        const float* mask, float scale, float* ctx, float* amax_slots,
                        const float* q_scale, int8_t* q_out, void* stream);
+
+/*
+ * ---- 4-bit microscaled FC layers, FC layers grouped by expert, routing ----
+ *
+ * The 4-bit format is MXFP4 of the OCP Microscaling Formats specification 1.0.  Blocks of 32 neighbours of a row share a power
+ * of two, 2^s with s = max(floor(log2 max|x|) - 2, -127), and an element is the E2M1 number nearest to x / 2^s -- one of 0, 0.5, 1,
+ * 1.5, 2, 3, 4, 6 with a sign; ties go to the number with an even mantissa, magnitudes above 6 to 6.  An all-zero block has s = -127;
+ * a block with an infinity or a NaN in it stands for 32 NaN.
+ *   A row of K elements is stored as G = ceil(K / 128) groups of 128, the elements behind the K-th zero:
+ *   codes  uint8[rows, 64 G]     element 2i in the low half of byte i, 2i + 1 in the high half: bit 3 the sign, 0 to 7 the numbers above
+ *   scales uint8[G, rows, 4]     s + 127 of the four blocks of a group; 255 is NaN.  Group by group, so that the scales of neighbouring
+ *                                rows lie side by side, as the matrix instructions take them.
+ * Codes have to be 16-byte aligned, scales 4-byte.  Weights [N, K] are quantized along K like activations; several matrices of
+ * the same shape (experts) are stored one behind the other: codes [n, N, 64 G], scales [n, G, N, 4].
+ * Outputs may not overlap inputs (Q8_ERR_OVERLAP) unless stated.  NaN and infinities in inputs are followed through these calls.
+ */
+#define Q8_MX4_MAX_K 1048576
+#define Q8_MX4_CODE_BYTES(K) (((int64_t)(K) + 127) / 128 * 64)   /* a row's codes */
+#define Q8_MX4_SCALE_BYTES(K) (((int64_t)(K) + 127) / 128 * 4)   /* a row's scales */
+
+/* Element types of the tensors passed as void*. */
+#define Q8_TYPE_F32 0
+#define Q8_TYPE_BF16 1
+#define Q8_TYPE_MX4 2   /* outputs of the 4-bit products: y receives codes, y_scales their scales */
+#define Q8_TYPE_I8 3    /* outputs of q8_linear_grouped under Q8_EPI_REQUANT */
+
+/*
+ * Codes and scales of x [M,K], in one pass.
+ *   x_type Q8_TYPE_F32 or Q8_TYPE_BF16.  M, K >= 0 (either 0: nothing written); K <= Q8_MX4_MAX_K.
+ */
+q8_status q8_mx4_quantize(const void* x, int x_type, int64_t M, int64_t K, uint8_t* codes, uint8_t* scales, void* stream);
+
+/*
+ * The quantizer of a training step: xq[m,k] = the value that the code of x[m,k] stands for (NaN in a block with an infinity or a NaN),
+ * exact in either type.  Its gradient is the straight-through estimator, q8_ste_backward.
+ *   x, xq of one type, Q8_TYPE_F32 or Q8_TYPE_BF16; xq may be x itself.
+ */
+q8_status q8_mx4_fake_quantize(const void* x, int type, int64_t M, int64_t K, void* xq, void* stream);
+
+/*
+ * The FC layer on 4-bit codes: y[m,n] = act(sum_k x[m,k] w[n,k] + bias[n]), products exact, sums in fp32.
+ *   xq, xs: codes and scales of x [M,K]; wq, ws: of w [N,K]; bias fp32[N] or NULL.
+ *   y_type Q8_TYPE_F32 or Q8_TYPE_BF16 (rounded once to nearest even): y [M,N], y_scales ignored.
+ *   y_type Q8_TYPE_MX4: N a multiple of 128; y and y_scales receive the codes and scales of the fp32 result, the same bytes that
+ *   q8_mx4_quantize makes of it, and the result itself is not stored: the next layer's quantizer costs no pass over memory.
+ *   flags: Q8_EPI_GELU or 0.
+ * M, N, K >= 0, K <= Q8_MX4_MAX_K, M * N <= 2^34.
+ */
+q8_status q8_mx4_linear(const uint8_t* xq, const uint8_t* xs, const uint8_t* wq, const uint8_t* ws, const float* bias, int64_t M,
+                        int64_t N, int64_t K, void* y, int y_type, uint8_t* y_scales, uint32_t flags, void* stream);
+
+/*
+ * The same on an fp32 or bf16 x [M,K], quantized on the way: the results of q8_mx4_quantize followed by q8_mx4_linear.
+ *   xq_work uint8[M * Q8_MX4_CODE_BYTES(K)] (16-byte aligned), xs_work uint8[M * Q8_MX4_SCALE_BYTES(K)] (4-byte aligned): scratch, contents
+ *   unspecified on return.
+ */
+q8_status q8_mx4_linear_dynamic(const void* x, int x_type, const uint8_t* wq, const uint8_t* ws, const float* bias, int64_t M, int64_t N,
+                                int64_t K, uint8_t* xq_work, uint8_t* xs_work, void* y, int y_type, uint8_t* y_scales, uint32_t flags,
+                                void* stream);
+
+/*
+ * FC layers of a mixture of experts on 4-bit codes.  The M rows of y belong to experts in order: the first group_rows[0] to expert 0, the
+ * next group_rows[1] to expert 1, ...
+ *     y[r,n] = act(sum_k x[x_rows[r],k] w[e(r),n,k] + bias[e(r),n])
+ *   xq, xs: codes and scales of x [x_count, K]; x_rows int32[M] the row of x that each row of y reads, or NULL: x has M rows and row r
+ *   reads row r.  An index outside x counts as a row of zeros; nothing is read out of bounds.
+ *   wq, ws: codes and scales of n_experts matrices [N,K]; bias fp32[n_experts, N] or NULL.
+ *   group_rows int32[n_experts], on the device, as q8_route leaves it.  Negative numbers count as zero, and rows beyond M do not exist:
+ *   whatever it holds, nothing outside y is written.  Rows of y behind the last group's stay as they are (a buffer may be larger than
+ *   the batch), and so do their scales where y holds 4-bit codes.
+ *   y, y_type, y_scales, flags as q8_mx4_linear.  1 <= n_experts <= Q8_MAX_EXPERTS; M * N <= 2^34.
+ */
+#define Q8_MAX_EXPERTS 65536
+q8_status q8_mx4_linear_grouped(const uint8_t* xq, const uint8_t* xs, int64_t x_count, const int32_t* x_rows, const uint8_t* wq,
+                                const uint8_t* ws, const float* bias, const int32_t* group_rows, int n_experts, int64_t M, int64_t N,
+                                int64_t K, void* y, int y_type, uint8_t* y_scales, uint32_t flags, void* stream);
+
+/*
+ * The same on int8 codes: each expert's rows as q8_linear has them, with the expert's own weights, scale and bias (one group of columns).
+ *   xq int8[x_count, K]; wq int8[n_experts, N, K]; bias fp32[n_experts, N] or NULL; sx fp32[1]; sw fp32[n_experts].
+ *   y fp32[M,N], or int8[M,N] with Q8_EPI_REQUANT; out_amax, next_scale and flags as q8_linear (the abs-max is that of the rows that
+ *   belong to an expert).  x_count, x_rows, group_rows as above.  0 <= K <= Q8_MAX_K, any alignment of the codes.
+ */
+q8_status q8_linear_grouped(const int8_t* xq, int64_t x_count, const int32_t* x_rows, const int8_t* wq, const float* bias, const float* sx,
+                            const float* sw, const int32_t* group_rows, int n_experts, int64_t M, int64_t N, int64_t K, void* y,
+                            float* out_amax, const float* next_scale, uint32_t flags, void* stream);
+
+/*
+ * The router of a mixture of experts: each token's k experts of largest logit, and its rows in the experts' order.
+ *   logits fp32[T, n_experts]; 1 <= n_experts <= Q8_ROUTE_MAX_EXPERTS, 1 <= k <= min(n_experts, Q8_ROUTE_MAX_K), T * k < 2^31.
+ *   experts int32[T,k]: by falling logit, ties by rising index.  -inf (an expert that is masked out) comes last, NaN counts as -inf.
+ *   gates fp32[T,k]: softmax over the k chosen logits; 0 for a logit of -inf, so all 0 for a token that has no other.  Several of +inf
+ *   share the gate.
+ *   group_rows int32[n_experts]: (token, choice) pairs of each expert.
+ *   rows int32[T*k]: the tokens of the pairs sorted by expert, within an expert by token: the x_rows of the grouped products.
+ *   slots int32[T,k]: where each pair went: rows[slots[t,j]] = t.
+ *   work int32[Q8_ROUTE_BLOCKS * n_experts]: scratch, contents unspecified on return.
+ *   T = 0 writes group_rows alone.
+ */
+#define Q8_ROUTE_MAX_EXPERTS 1024
+#define Q8_ROUTE_MAX_K 16
+#define Q8_ROUTE_BLOCKS 256
+q8_status q8_route(const float* logits, int64_t T, int n_experts, int k, int32_t* experts, float* gates, int32_t* group_rows, int32_t* rows,
+                   int32_t* slots, int32_t* work, void* stream);
+
+/*
+ * The sum behind the experts: out[t,:] = sum_j gates[t,j] y[slots[t,j],:], in fp32 in the order of j, rounded once to out's type.
+ *   y [R,N] and out [T,N] of one type, Q8_TYPE_F32 or Q8_TYPE_BF16; slots int32[T,k], gates fp32[T,k].  A slot outside [0,R) adds nothing.
+ *   T, R, N >= 0; k >= 1.
+ */
+q8_status q8_combine(const void* y, int64_t R, const int32_t* slots, const float* gates, int64_t T, int k, int64_t N, void* out, int type,
+                     void* stream);
 
 /*
  * ---- tuning / debugging (not part of the method) ----

@@ -108,6 +108,65 @@ bool few_tokens_overlap(const float* x, const int8_t* wq, const q8::Epilogue& ep
     return false;
 }
 
+// ---- 4-bit and grouped products ----
+
+bool float_type(int t) { return t == Q8_TYPE_F32 || t == Q8_TYPE_BF16; }
+int64_t type_bytes(int t) { return t == Q8_TYPE_F32 ? 4 : t == Q8_TYPE_BF16 ? 2 : 1; }
+
+constexpr int64_t kMaxOutputs = (int64_t)1 << 34, kMaxRows = 0x7fffffff;
+
+// Sizes and pointers that the 4-bit and the int8 products have in common, and what may not overlap.
+q8_status check_product(bool mx4, const q8::Product& p, int64_t K)
+{
+    if (p.M < 0 || p.N < 0 || K < 0 || K > (mx4 ? Q8_MX4_MAX_K : Q8_MAX_K) || p.x_count < 0) return Q8_ERR_SHAPE;
+    if (p.n_groups < 1 || p.n_groups > Q8_MAX_EXPERTS) return Q8_ERR_SHAPE;
+    if (p.M > kMaxRows || p.N > kMaxRows || p.x_count > kMaxRows || (p.N > 0 && p.M > kMaxOutputs / p.N)) return Q8_ERR_SHAPE;
+    if (p.N > 0 && p.n_groups > kMaxOutputs / p.N) return Q8_ERR_SHAPE;
+    if (p.M == 0 || p.N == 0) return Q8_OK;
+    if (p.x_rows ? p.x_count < 1 : p.x_count != p.M) return Q8_ERR_SHAPE;
+    if (!p.y || (K > 0 && (!p.x || !p.w))) return Q8_ERR_NULL;
+    if (misaligned(p.x_rows, 4) || misaligned(p.group_rows, 4) || misaligned(p.bias, 4)) return Q8_ERR_ALIGN;
+    const int64_t y_bytes = p.y_type == Q8_TYPE_MX4 ? p.M * Q8_MX4_CODE_BYTES(p.N) : p.M * p.N * (p.y_type == Q8_TYPE_BF16 ? 2 : p.y_type == Q8_TYPE_F32 ? 4 : 1);
+    const int64_t ys_bytes = p.y_type == Q8_TYPE_MX4 ? p.M * Q8_MX4_SCALE_BYTES(p.N) : 0, w_rows = (int64_t)p.n_groups * p.N;
+    const struct { const void* p; int64_t bytes; } in[] = {
+        {p.x, p.x_count * p.pitch}, {p.w, w_rows * p.pitch}, {p.xs, p.x_count * (p.pitch / 16)}, {p.ws, w_rows * (p.pitch / 16)},
+        {p.x_rows, 4 * p.M}, {p.group_rows, 4 * (int64_t)p.n_groups}, {p.bias, 4 * w_rows}, {p.sx, 4}, {p.sw, 4 * (int64_t)p.n_groups},
+        {p.next_scale, 4}, {p.out_amax, 4}};
+    for (const auto& r : in)
+        if (overlap(r.p, r.bytes, p.y, y_bytes) || (ys_bytes && overlap(r.p, r.bytes, p.y_scales, ys_bytes))) return Q8_ERR_OVERLAP;
+    if (ys_bytes && overlap(p.y, y_bytes, p.y_scales, ys_bytes)) return Q8_ERR_OVERLAP;
+    return Q8_OK;
+}
+
+q8_status check_mx4_product(const q8::Product& p, int64_t K)
+{
+    if (p.flags & ~Q8_EPI_GELU) return Q8_ERR_FLAGS;
+    if (!float_type(p.y_type) && p.y_type != Q8_TYPE_MX4) return Q8_ERR_FLAGS;
+    const bool to_codes = p.y_type == Q8_TYPE_MX4;
+    if (to_codes && p.N % 128 != 0) return Q8_ERR_SHAPE;
+    if (p.M > 0 && p.N > 0 && ((to_codes && !p.y_scales) || (K > 0 && (!p.xs || !p.ws)))) return Q8_ERR_NULL;
+    if (misaligned(p.x, 16) || misaligned(p.w, 16) || misaligned(p.xs, 4) || misaligned(p.ws, 4)) return Q8_ERR_ALIGN;
+    if (misaligned(p.y, to_codes ? 16 : p.y_type == Q8_TYPE_BF16 ? 2 : 4) || (to_codes && misaligned(p.y_scales, 4))) return Q8_ERR_ALIGN;
+    return check_product(true, p, K);
+}
+
+q8::Product mx4_product(const uint8_t* xq, const uint8_t* xs, int64_t x_count, const int32_t* x_rows, const uint8_t* wq, const uint8_t* ws, const float* bias,
+                        const int32_t* group_rows, int n_groups, int64_t M, int64_t N, int64_t K, void* y, int y_type, uint8_t* y_scales, uint32_t flags)
+{
+    q8::Product p{};
+    p.x = xq, p.xs = xs, p.x_rows = x_rows, p.x_count = x_count;
+    p.w = wq, p.ws = ws, p.bias = bias, p.group_rows = group_rows, p.n_groups = n_groups;
+    p.M = M, p.N = N, p.pitch = K > 0 ? Q8_MX4_CODE_BYTES(K) : 0;
+    p.y = y, p.y_type = y_type, p.y_scales = y_scales, p.flags = flags;
+    return p;
+}
+
+// M and K of a tensor to be quantized to 4 bits: the limit on their product is the launch's.
+bool bad_mx4_shape(int64_t M, int64_t K)
+{
+    return M < 0 || K < 0 || K > Q8_MX4_MAX_K || M > kMaxRows || (K > 0 && (M + 15) / 16 > (((int64_t)1 << 24) - 1) / ((K + 127) / 128));
+}
+
 }  // namespace
 
 extern "C" {
@@ -385,6 +444,119 @@ q8_status q8_attention(const float* qkv, int64_t B, int64_t S, int heads, int d,
                : Q8_OK;
 }
 
+q8_status q8_mx4_quantize(const void* x, int x_type, int64_t M, int64_t K, uint8_t* codes, uint8_t* scales, void* stream)
+{
+    if (bad_mx4_shape(M, K)) return Q8_ERR_SHAPE;
+    if (!float_type(x_type)) return Q8_ERR_FLAGS;
+    if (M == 0 || K == 0) return Q8_OK;
+    if (!x || !codes || !scales) return Q8_ERR_NULL;
+    if (misaligned(x, (unsigned)type_bytes(x_type)) || misaligned(codes, 16) || misaligned(scales, 4)) return Q8_ERR_ALIGN;
+    const int64_t x_bytes = M * K * type_bytes(x_type), c_bytes = M * Q8_MX4_CODE_BYTES(K), s_bytes = M * Q8_MX4_SCALE_BYTES(K);
+    if (overlap(x, x_bytes, codes, c_bytes) || overlap(x, x_bytes, scales, s_bytes) || overlap(codes, c_bytes, scales, s_bytes)) return Q8_ERR_OVERLAP;
+    return q8::launch_mx4_quantize(x, x_type == Q8_TYPE_BF16, M, K, codes, scales, as_stream(stream)) ? Q8_ERR_LAUNCH : Q8_OK;
+}
+
+q8_status q8_mx4_fake_quantize(const void* x, int type, int64_t M, int64_t K, void* xq, void* stream)
+{
+    if (bad_mx4_shape(M, K)) return Q8_ERR_SHAPE;
+    if (!float_type(type)) return Q8_ERR_FLAGS;
+    if (M == 0 || K == 0) return Q8_OK;
+    if (!x || !xq) return Q8_ERR_NULL;
+    if (misaligned(x, (unsigned)type_bytes(type)) || misaligned(xq, (unsigned)type_bytes(type))) return Q8_ERR_ALIGN;
+    if (x != xq && overlap(x, M * K * type_bytes(type), xq, M * K * type_bytes(type))) return Q8_ERR_OVERLAP;
+    return q8::launch_mx4_fake_quantize(x, type == Q8_TYPE_BF16, M, K, xq, as_stream(stream)) ? Q8_ERR_LAUNCH : Q8_OK;
+}
+
+q8_status q8_mx4_linear(const uint8_t* xq, const uint8_t* xs, const uint8_t* wq, const uint8_t* ws, const float* bias, int64_t M, int64_t N, int64_t K,
+                        void* y, int y_type, uint8_t* y_scales, uint32_t flags, void* stream)
+{
+    const q8::Product p = mx4_product(xq, xs, M, nullptr, wq, ws, bias, nullptr, 1, M, N, K, y, y_type, y_scales, flags);
+    const q8_status s = check_mx4_product(p, K);
+    if (s != Q8_OK || M == 0 || N == 0) return s;
+    return q8::launch_product(true, p, as_stream(stream)) ? Q8_ERR_LAUNCH : Q8_OK;
+}
+
+q8_status q8_mx4_linear_dynamic(const void* x, int x_type, const uint8_t* wq, const uint8_t* ws, const float* bias, int64_t M, int64_t N, int64_t K,
+                                uint8_t* xq_work, uint8_t* xs_work, void* y, int y_type, uint8_t* y_scales, uint32_t flags, void* stream)
+{
+    if (bad_mx4_shape(M, K)) return Q8_ERR_SHAPE;
+    if (!float_type(x_type)) return Q8_ERR_FLAGS;
+    const q8::Product p = mx4_product(xq_work, xs_work, M, nullptr, wq, ws, bias, nullptr, 1, M, N, K, y, y_type, y_scales, flags);
+    q8_status s = check_mx4_product(p, K);
+    if (s != Q8_OK || M == 0 || N == 0) return s;
+    if (K > 0) {
+        // the quantizer writes the scratch while w and bias still have to be read
+        const int64_t c_bytes = M * p.pitch, s_bytes = M * (p.pitch / 16);
+        const struct { const void* p; int64_t bytes; } read[] = {{wq, N * p.pitch}, {ws, N * (p.pitch / 16)}, {bias, 4 * N}};
+        for (const auto& r : read)
+            if (overlap(r.p, r.bytes, xq_work, c_bytes) || overlap(r.p, r.bytes, xs_work, s_bytes)) return Q8_ERR_OVERLAP;
+        const int64_t x_bytes = M * K * type_bytes(x_type), y_bytes = y_type == Q8_TYPE_MX4 ? M * Q8_MX4_CODE_BYTES(N) : M * N * type_bytes(y_type);
+        if (overlap(x, x_bytes, y, y_bytes) || (y_type == Q8_TYPE_MX4 && overlap(x, x_bytes, y_scales, M * Q8_MX4_SCALE_BYTES(N)))) return Q8_ERR_OVERLAP;
+        s = q8_mx4_quantize(x, x_type, M, K, xq_work, xs_work, stream);
+        if (s != Q8_OK) return s;
+    }
+    return q8::launch_product(true, p, as_stream(stream)) ? Q8_ERR_LAUNCH : Q8_OK;
+}
+
+q8_status q8_mx4_linear_grouped(const uint8_t* xq, const uint8_t* xs, int64_t x_count, const int32_t* x_rows, const uint8_t* wq, const uint8_t* ws,
+                                const float* bias, const int32_t* group_rows, int n_experts, int64_t M, int64_t N, int64_t K, void* y, int y_type,
+                                uint8_t* y_scales, uint32_t flags, void* stream)
+{
+    const q8::Product p = mx4_product(xq, xs, x_count, x_rows, wq, ws, bias, group_rows, n_experts, M, N, K, y, y_type, y_scales, flags);
+    const q8_status s = check_mx4_product(p, K);
+    if (s != Q8_OK || M == 0 || N == 0) return s;
+    if (!group_rows) return Q8_ERR_NULL;
+    return q8::launch_product(true, p, as_stream(stream)) ? Q8_ERR_LAUNCH : Q8_OK;
+}
+
+q8_status q8_linear_grouped(const int8_t* xq, int64_t x_count, const int32_t* x_rows, const int8_t* wq, const float* bias, const float* sx, const float* sw,
+                            const int32_t* group_rows, int n_experts, int64_t M, int64_t N, int64_t K, void* y, float* out_amax, const float* next_scale,
+                            uint32_t flags, void* stream)
+{
+    if (flags & ~kKnownFlags) return Q8_ERR_FLAGS;
+    if ((flags & Q8_EPI_ABSMAX) && !out_amax) return Q8_ERR_FLAGS;
+    if ((flags & Q8_EPI_REQUANT) && !next_scale) return Q8_ERR_FLAGS;
+    q8::Product p{};
+    p.x = reinterpret_cast<const uint8_t*>(xq), p.x_rows = x_rows, p.x_count = x_count;
+    p.w = reinterpret_cast<const uint8_t*>(wq), p.bias = bias, p.group_rows = group_rows, p.n_groups = n_experts;
+    p.M = M, p.N = N, p.pitch = K, p.sx = sx, p.sw = sw;
+    p.y = y, p.y_type = (flags & Q8_EPI_REQUANT) ? Q8_TYPE_I8 : Q8_TYPE_F32, p.flags = flags;
+    p.next_scale = (flags & Q8_EPI_REQUANT) ? next_scale : nullptr, p.out_amax = (flags & Q8_EPI_ABSMAX) ? out_amax : nullptr;
+    if (misaligned(sx, 4) || misaligned(sw, 4) || misaligned(p.out_amax, 4) || misaligned(p.next_scale, 4)) return Q8_ERR_ALIGN;
+    if (p.y_type == Q8_TYPE_F32 && misaligned(y, 4)) return Q8_ERR_ALIGN;
+    const q8_status s = check_product(false, p, K);
+    if (s != Q8_OK || M == 0 || N == 0) return s;
+    if (!sx || !sw || !group_rows) return Q8_ERR_NULL;
+    return q8::launch_product(false, p, as_stream(stream)) ? Q8_ERR_LAUNCH : Q8_OK;
+}
+
+q8_status q8_route(const float* logits, int64_t T, int n_experts, int k, int32_t* experts, float* gates, int32_t* group_rows, int32_t* rows, int32_t* slots,
+                   int32_t* work, void* stream)
+{
+    if (T < 0 || n_experts < 1 || n_experts > Q8_ROUTE_MAX_EXPERTS || k < 1 || k > n_experts || k > Q8_ROUTE_MAX_K || T > kMaxRows / k) return Q8_ERR_SHAPE;
+    if (!group_rows || !work || (T > 0 && (!logits || !experts || !gates || !rows || !slots))) return Q8_ERR_NULL;
+    const struct { const void* p; int64_t bytes; } part[] = {{logits, 4 * T * n_experts}, {experts, 4 * T * k}, {gates, 4 * T * k}, {group_rows, 4 * (int64_t)n_experts},
+                                                             {rows, 4 * T * k}, {slots, 4 * T * k}, {work, 4 * (int64_t)Q8_ROUTE_BLOCKS * n_experts}};
+    for (const auto& a : part) {
+        if (misaligned(a.p, 4)) return Q8_ERR_ALIGN;
+        for (const auto& b : part)
+            if (&a < &b && overlap(a.p, a.bytes, b.p, b.bytes)) return Q8_ERR_OVERLAP;
+    }
+    return q8::launch_route(logits, T, n_experts, k, experts, gates, group_rows, rows, slots, work, as_stream(stream)) ? Q8_ERR_LAUNCH : Q8_OK;
+}
+
+q8_status q8_combine(const void* y, int64_t R, const int32_t* slots, const float* gates, int64_t T, int k, int64_t N, void* out, int type, void* stream)
+{
+    if (R < 0 || T < 0 || N < 0 || k < 1 || R > kMaxRows || T > kMaxRows / k || (N > 0 && (T > kMaxOutputs / N / 8 || R > ((int64_t)1 << 40) / N))) return Q8_ERR_SHAPE;
+    if (!float_type(type)) return Q8_ERR_FLAGS;
+    if (T == 0 || N == 0) return Q8_OK;
+    if ((R > 0 && !y) || !slots || !gates || !out) return Q8_ERR_NULL;
+    if (misaligned(y, (unsigned)type_bytes(type)) || misaligned(out, (unsigned)type_bytes(type)) || misaligned(slots, 4) || misaligned(gates, 4)) return Q8_ERR_ALIGN;
+    const int64_t out_bytes = T * N * type_bytes(type);
+    if (overlap(y, R * N * type_bytes(type), out, out_bytes) || overlap(slots, 4 * T * k, out, out_bytes) || overlap(gates, 4 * T * k, out, out_bytes)) return Q8_ERR_OVERLAP;
+    return q8::launch_combine(y, R, slots, gates, T, k, N, out, type == Q8_TYPE_BF16, as_stream(stream)) ? Q8_ERR_LAUNCH : Q8_OK;
+}
+
 const char* q8_version(void) { return "q8 0.1.0 (gfx950)"; }
 
 const char* q8_status_str(q8_status s)
@@ -397,6 +569,7 @@ const char* q8_status_str(q8_status s)
         case Q8_ERR_FLAGS: return "bad epilogue flags";
         case Q8_ERR_LAUNCH: return "launch failed";
         case Q8_ERR_TOO_LARGE: return "input exceeds the static scratch of the no-allocation entry point";
+        case Q8_ERR_OVERLAP: return "an output overlaps an input or another output";
     }
     return "unknown status";
 }

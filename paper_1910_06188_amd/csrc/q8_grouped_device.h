@@ -1,0 +1,133 @@
+// What the kernels of the grouped products share: the two kinds of operands, where a workgroup's rows are, and the epilogue.
+#pragma once
+#include "q8.h"
+#include "q8_device.h"
+#include "q8_epilogue.h"
+#include "q8_launch.h"
+#include "q8_mx4_device.h"
+
+namespace q8 {
+
+typedef int v8i __attribute__((ext_vector_type(8)));
+typedef float v16f __attribute__((ext_vector_type(16)));
+
+// One MFMA takes 32 bytes of 32 rows of either operand, 16 bytes a lane: 32 int8 codes, or 64 4-bit codes of which a lane holds
+// one block with its scale.  So both kinds move through memory, LDS and registers alike, in units of 128 bytes of a row, and only
+// the instruction, the accumulator's type and the scales differ.
+//
+// A lane's 16 bytes of step s of a unit are chunk 4 (lane / 32) + s, not 2 s + lane / 32 as the instruction numbers them: a sum does
+// not mind the order of its terms as long as both operands have the same one, and this way the four scales that a lane needs for a unit
+// are the four bytes of one group's word, one for each step, which the instruction picks by a constant.
+struct OpI8 {
+    static constexpr bool kMx4 = false;
+    using Acc = v16i;
+    using Sum = int;
+    template <int kStep>
+    static __device__ __forceinline__ Acc mfma(v4i a, v4i b, Acc c, int, int)
+    {
+        return __builtin_amdgcn_mfma_i32_32x32x32_i8(a, b, c, 0, 0, 0);
+    }
+};
+struct OpMx4 {
+    static constexpr bool kMx4 = true;
+    using Acc = v16f;
+    using Sum = float;
+    template <int kStep>
+    static __device__ __forceinline__ Acc mfma(v4i a, v4i b, Acc c, int sa, int sb)
+    {
+        const v8i a8 = {a[0], a[1], a[2], a[3], 0, 0, 0, 0}, b8 = {b[0], b[1], b[2], b[3], 0, 0, 0, 0};
+        return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a8, b8, c, 4, 4, kStep, sa, kStep, sb);  // format 4: E2M1
+    }
+};
+
+// Inclusive scan over the 64 lanes of a + b, at most `most` (< 2^31) and so never above 32 bits; truncated addition is associative.
+template <int kCtrl, int kRowMask>
+__device__ __forceinline__ unsigned dpp_add_most(unsigned v, unsigned most)
+{
+    return min(v + (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, kCtrl, kRowMask, 0xf, true), most);
+}
+__device__ __forceinline__ unsigned wave_scan_most(unsigned v, unsigned most)
+{
+    v = dpp_add_most<0x111, 0xf>(v, most);  // row_shr:1
+    v = dpp_add_most<0x112, 0xf>(v, most);
+    v = dpp_add_most<0x114, 0xf>(v, most);
+    v = dpp_add_most<0x118, 0xf>(v, most);
+    v = dpp_add_most<0x142, 0xa>(v, most);  // row_bcast:15
+    v = dpp_add_most<0x143, 0xc>(v, most);  // row_bcast:31
+    return v;
+}
+
+// The t-th tile of kRows rows that stay inside a group: its group, its first row of y, its rows (0: there is no such tile).
+// Rows are dealt out in order and only as far as y goes, and a negative number of rows counts as none, so that whatever group_rows
+// holds no two groups share a row and none leaves y.  Every wave finds its tile by itself: the counts of 64 groups a pass, one a
+// lane, and two scans in the vector ALU.
+struct RowTile {
+    int group, row, rows;
+};
+template <int kRows>
+__device__ __forceinline__ RowTile find_row_tile(const int32_t* __restrict__ group_rows, int n_groups, int M, unsigned t)
+{
+    if (!group_rows) {
+        const int row = (int)(t * kRows);
+        return RowTile{0, row, min(kRows, M - row)};
+    }
+    const int lane = threadIdx.x & 63;
+    unsigned before = 0;  // rows of the groups already passed
+    for (int g0 = 0; g0 < n_groups; g0 += 64) {
+        const int n = g0 + lane < n_groups ? min(max(group_rows[g0 + lane], 0), M) : 0;
+        const unsigned upto = min(before + wave_scan_most((unsigned)n, (unsigned)M), (unsigned)M);
+        const unsigned prev = (unsigned)__shfl_up((int)upto, 1);
+        const unsigned start = lane ? prev : before;
+        const unsigned tiles = (upto - start + kRows - 1) / kRows, ends = wave_scan_most(tiles, 0x7fffffffu);
+        const unsigned long long behind = __ballot(t < ends);
+        if (behind) {
+            const int l = __builtin_ctzll(behind);
+            const unsigned first = (unsigned)__builtin_amdgcn_readlane((int)(ends - tiles), l);
+            const int row = __builtin_amdgcn_readlane((int)start, l) + (int)((t - first) * kRows);
+            return RowTile{g0 + l, row, min(kRows, __builtin_amdgcn_readlane((int)upto, l) - row)};
+        }
+        t -= (unsigned)__builtin_amdgcn_readlane((int)ends, 63);
+        before = (unsigned)__builtin_amdgcn_readlane((int)upto, 63);
+    }
+    return RowTile{0, 0, 0};
+}
+
+// Tiles of kRows rows that M rows in n_groups groups can have at most: every group that has rows may end inside a tile.
+inline int64_t row_tiles(int64_t M, const int32_t* group_rows, int64_t n_groups, int64_t rows)
+{
+    const int64_t ragged = group_rows ? (n_groups < M ? n_groups : M) : 1;
+    return (M + ragged * (rows - 1)) / rows;
+}
+
+// Per-column constants and the value of an output.
+struct ProductColumn {
+    int bq;       // int8: quantized bias
+    float r, b;   // int8: 1 / (S_x S_W); 4-bit: the bias
+};
+template <class Op>
+__device__ __forceinline__ ProductColumn product_column(const Product& p, int group, int64_t n, float sx)
+{
+    const float b = p.bias ? p.bias[(int64_t)group * p.N + n] : 0.0f;
+    if constexpr (Op::kMx4) return ProductColumn{0, 1.0f, b};
+    const float sw = p.sw[group];
+    return ProductColumn{p.bias ? quantize_bias(b, sx, sw) : 0, dequant_factor(sx, sw), 0.0f};
+}
+template <class Op>
+__device__ __forceinline__ float product_value(typename Op::Sum sum, const ProductColumn& c)
+{
+    if constexpr (Op::kMx4)
+        return __fadd_rn(sum, c.b);
+    else
+        return (float)(sum + c.bq) * c.r;
+}
+
+// Maximum over each half of 32 lanes.
+__device__ __forceinline__ unsigned half_wave_max_u32(unsigned v)
+{
+    v = quad_max_u32(v);
+    v = max(v, (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, 0x141, 0xf, 0xf, true));  // row_half_mirror
+    v = max(v, (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, 0x140, 0xf, 0xf, true));  // row_mirror
+    return max(v, (unsigned)__shfl_xor((int)v, 16));
+}
+
+}  // namespace q8

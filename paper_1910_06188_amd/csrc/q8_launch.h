@@ -64,6 +64,42 @@ bool fc_small_eligible(const float* x, const int8_t* wq, int64_t M, int64_t N, i
 int launch_fc_small(const float* x, const int8_t* wq, int64_t M, int64_t N, int64_t K, int8_t* xq_out, float* scal_out,
                     const Epilogue& ep, hipStream_t st);
 
+// Quantization to the 4-bit microscaled format, and to the values of its codes (q8_mx4.hip).
+int launch_mx4_quantize(const void* x, bool bf16, int64_t M, int64_t K, uint8_t* codes, uint8_t* scales, hipStream_t st);
+int launch_mx4_fake_quantize(const void* x, bool bf16, int64_t M, int64_t K, void* xq, hipStream_t st);
+
+// FC products whose rows belong to groups (experts) with weights of their own, on int8 or on 4-bit microscaled codes; a plain
+// 4-bit layer is one group of all rows (q8_grouped.hip).
+struct Product {
+    const uint8_t* x;            // codes, rows of `pitch` bytes
+    const uint8_t* xs;           // 4-bit: scales [groups of 128][x_count][4]
+    const int32_t* x_rows;       // row of x for each row of y, or null: the same
+    int64_t x_count;             // rows of x
+    const uint8_t* w;            // codes [n_groups][N], rows of `pitch` bytes
+    const uint8_t* ws;           // 4-bit: scales [n_groups][groups of 128][N][4]
+    const int32_t* group_rows;   // rows of each group, or null: one group of M
+    int n_groups;
+    int64_t M, N, pitch;
+    const float* bias;           // fp32[n_groups][N] or null
+    const float* sx;             // int8: fp32[1]
+    const float* sw;             // int8: fp32[n_groups]
+    const float* next_scale;     // int8: fp32[1] or null
+    float* out_amax;             // int8: fp32[1] or null
+    void* y;
+    uint8_t* y_scales;           // 4-bit y: scales [N / 128][M][4]
+    int y_type;                  // Q8_TYPE_*
+    unsigned flags;
+};
+int launch_product(bool mx4, const Product& p, hipStream_t st);
+// 32x32 tiles for any size and alignment (q8_grouped_direct.hip).
+int launch_product_direct(bool mx4, const Product& p, hipStream_t st);
+
+// The router of a mixture of experts and the sum behind it (q8_route.hip).
+int launch_route(const float* logits, int64_t T, int n_experts, int k, int32_t* experts, float* gates, int32_t* group_rows, int32_t* rows,
+                 int32_t* slots, int32_t* work, hipStream_t st);
+int launch_combine(const void* y, int64_t R, const int32_t* slots, const float* gates, int64_t T, int k, int64_t N, void* out, bool bf16,
+                   hipStream_t st);
+
 int launch_embedding(const int8_t* table, const float* scale, int64_t V, int64_t H, const int32_t* ids, int64_t T,
                      void* out, int out_is_int8, int32_t* err_flag, hipStream_t st);
 int launch_embedding_sum3(const int8_t* word, int64_t Vw, const int8_t* pos, int64_t Vp, const int8_t* type,

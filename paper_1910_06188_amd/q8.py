@@ -34,6 +34,9 @@ MAX_K = 131071
 STATIC_MAX_CODES = 64 << 20
 SCAL_WORK = 2050
 AMAX_SLOTS = 2048
+MX4_MAX_K = 1048576
+TYPE_F32, TYPE_BF16, TYPE_MX4, TYPE_I8 = 0, 1, 2, 3
+ROUTE_BLOCKS, ROUTE_MAX_EXPERTS, ROUTE_MAX_K = 256, 1024, 16
 
 _vp, _i64, _i32, _u32 = C.c_void_p, C.c_int64, C.c_int, C.c_uint32
 
@@ -67,6 +70,17 @@ _lib.q8_debug_stream_copy.restype = C.c_int
 _lib.q8_debug_loop_probe.argtypes = [_i32, _vp, _vp, _i32, _vp, _vp]
 _lib.q8_debug_loop_probe.restype = C.c_int
 _lib.q8_linear_f32_slots.argtypes = [_vp, _vp, _i32, _vp, _vp, _vp, _i32, _i64, _i64, _i64, _vp, _vp, _vp, _vp, _vp, _vp, _u32, _vp]
+_lib.q8_mx4_quantize.argtypes = [_vp, _i32, _i64, _i64, _vp, _vp, _vp]
+_lib.q8_mx4_fake_quantize.argtypes = [_vp, _i32, _i64, _i64, _vp, _vp]
+_lib.q8_mx4_linear.argtypes = [_vp, _vp, _vp, _vp, _vp, _i64, _i64, _i64, _vp, _i32, _vp, _u32, _vp]
+_lib.q8_mx4_linear_dynamic.argtypes = [_vp, _i32, _vp, _vp, _vp, _i64, _i64, _i64, _vp, _vp, _vp, _i32, _vp, _u32, _vp]
+_lib.q8_mx4_linear_grouped.argtypes = [_vp, _vp, _i64, _vp, _vp, _vp, _vp, _vp, _i32, _i64, _i64, _i64, _vp, _i32, _vp, _u32, _vp]
+_lib.q8_linear_grouped.argtypes = [_vp, _i64, _vp, _vp, _vp, _vp, _vp, _vp, _i32, _i64, _i64, _i64, _vp, _vp, _vp, _u32, _vp]
+_lib.q8_route.argtypes = [_vp, _i64, _i32, _i32, _vp, _vp, _vp, _vp, _vp, _vp, _vp]
+_lib.q8_combine.argtypes = [_vp, _i64, _vp, _vp, _i64, _i32, _i64, _vp, _i32, _vp]
+for _f in ("q8_mx4_quantize", "q8_mx4_fake_quantize", "q8_mx4_linear", "q8_mx4_linear_dynamic", "q8_mx4_linear_grouped", "q8_linear_grouped",
+           "q8_route", "q8_combine"):
+    getattr(_lib, _f).restype = C.c_int
 for _f in ("q8_linear_f32_slots", "q8_attention", "q8_layernorm_absmax", "q8_embedding_sum3_layernorm", "q8_fake_quantize", "q8_ema_update", "q8_fake_quantize_ema", "q8_ste_backward", "q8_absmax", "q8_scale_from_amax", "q8_quantize", "q8_quantize_amax", "q8_linear", "q8_linear_f32", "q8_embedding",
            "q8_embedding_sum3"):
     getattr(_lib, _f).restype = C.c_int
@@ -347,6 +361,132 @@ def q8_attention(qkv, B, S, heads, d, ctx=None, mask=None, scale=None, amax_slot
         scale = 1.0 / float(d) ** 0.5
     _ck(_binding.q8_attention(qkv, B, S, heads, d, mask, float(scale), ctx, amax_slots, q_scale,
                           q_out, _stream(stream)), "q8_attention")
+
+
+# ---- 4-bit microscaled FC layers, FC layers grouped by expert, routing --------------------------------------------------
+
+_FLOAT_TYPES = {torch.float32: TYPE_F32, torch.bfloat16: TYPE_BF16}
+
+
+def _float_type(t, where: str) -> int:
+    code = _FLOAT_TYPES.get(t.dtype)
+    if code is None:
+        raise TypeError(f"{where}: takes float32 or bfloat16, not {t.dtype}")
+    return code
+
+
+def mx4_empty(*shape, device="cuda"):
+    """Uninitialised codes and scales of a 4-bit tensor [rows, K], or of n of them [n, rows, K]."""
+    *lead, rows, K = shape
+    groups = (K + 127) // 128
+    return (torch.empty((*lead, rows, 64 * groups), dtype=torch.uint8, device=device),
+            torch.empty((*lead, groups, rows, 4), dtype=torch.uint8, device=device))
+
+
+def _mx4_bad(codes, scales) -> bool:
+    """Whether codes [..., rows, 64 G] and scales [..., G, rows, 4] do not fit each other."""
+    return (codes.dim() < 2 or codes.shape[-1] % 64 != 0 or
+            tuple(scales.shape) != (*codes.shape[:-2], codes.shape[-1] // 64, codes.shape[-2], 4))
+
+
+def _product_output(y, y_scales, M, N, where: str) -> int:
+    """The type code of a 4-bit product's output: codes if there are scales for them, else fp32 or bf16."""
+    if y_scales is None:
+        if tuple(y.shape) != (M, N):
+            raise ValueError(f"{where}: y is [{M}, {N}]")
+        return _float_type(y, where)
+    if y.dtype != torch.uint8:
+        raise TypeError(f"{where}: codes are uint8")
+    if N % 128 != 0 or tuple(y.shape) != (M, N // 2) or _mx4_bad(y, y_scales):
+        raise ValueError(f"{where}: 4-bit outputs are codes [{M}, {N} / 2] and scales [{N} / 128, {M}, 4] of a width that is a multiple of 128")
+    return TYPE_MX4
+
+
+def q8_mx4_quantize(x, codes, scales, stream=None) -> None:
+    """codes, scales = the 4-bit microscaled form of x [M, K] (fp32 or bf16); see mx4_empty."""
+    M, K = x.shape
+    if codes.shape[-1] != (K + 127) // 128 * 64 or codes.dim() != 2 or codes.shape[0] != M or _mx4_bad(codes, scales):
+        raise ValueError("q8_mx4_quantize: codes and scales do not fit x")
+    _ck(_binding.q8_mx4_quantize(x, _float_type(x, "q8_mx4_quantize"), M, K, codes, scales, _stream(stream)), "q8_mx4_quantize")
+
+
+def q8_mx4_fake_quantize(x, xq, stream=None) -> None:
+    """xq = the values that the 4-bit codes of x [M, K] stand for, in x's type; xq may be x.  Its gradient is q8_ste_backward."""
+    M, K = x.shape
+    if xq.shape != x.shape or xq.dtype != x.dtype:
+        raise ValueError("q8_mx4_fake_quantize: xq and x differ in shape or type")
+    _ck(_binding.q8_mx4_fake_quantize(x, _float_type(x, "q8_mx4_fake_quantize"), M, K, xq, _stream(stream)), "q8_mx4_fake_quantize")
+
+
+def q8_mx4_linear(xq, xs, wq, ws, bias, y, y_scales=None, flags=0, stream=None) -> None:
+    """y = act(x w^T + bias) on 4-bit codes and scales of x and w; y fp32, bf16, or (with y_scales) 4-bit codes itself."""
+    if xq.dim() != 2 or wq.dim() != 2 or _mx4_bad(xq, xs) or _mx4_bad(wq, ws) or xq.shape[1] != wq.shape[1]:
+        raise ValueError("q8_mx4_linear: shape mismatch")
+    M, N, K = xq.shape[0], wq.shape[0], 2 * xq.shape[1]
+    if bias is not None and bias.numel() != N:
+        raise ValueError("q8_mx4_linear: bias size mismatch")
+    y_type = _product_output(y, y_scales, M, N, "q8_mx4_linear")
+    _ck(_binding.q8_mx4_linear(xq, xs, wq, ws, bias, M, N, K, y, y_type, y_scales, flags, _stream(stream)), "q8_mx4_linear")
+
+
+def q8_mx4_linear_dynamic(x, wq, ws, bias, xq_work, xs_work, y, y_scales=None, flags=0, stream=None) -> None:
+    """q8_mx4_linear of an fp32 or bf16 x [M, K], quantized on the way (xq_work, xs_work: scratch as mx4_empty(M, K) makes it)."""
+    M, K = x.shape
+    if wq.dim() != 2 or _mx4_bad(wq, ws) or wq.shape[1] != (K + 127) // 128 * 64:
+        raise ValueError("q8_mx4_linear_dynamic: shape mismatch")
+    if xq_work.numel() < M * wq.shape[1] or xs_work.numel() < M * wq.shape[1] // 16 or xq_work.dtype != torch.uint8 or xs_work.dtype != torch.uint8:
+        raise ValueError("q8_mx4_linear_dynamic: scratch of mx4_empty(M, K) needed")
+    N = wq.shape[0]
+    if bias is not None and bias.numel() != N:
+        raise ValueError("q8_mx4_linear_dynamic: bias size mismatch")
+    y_type = _product_output(y, y_scales, M, N, "q8_mx4_linear_dynamic")
+    _ck(_binding.q8_mx4_linear_dynamic(x, _float_type(x, "q8_mx4_linear_dynamic"), wq, ws, bias, M, N, K, xq_work, xs_work, y, y_type, y_scales, flags,
+                                       _stream(stream)), "q8_mx4_linear_dynamic")
+
+
+def q8_mx4_linear_grouped(xq, xs, wq, ws, bias, group_rows, y, x_rows=None, y_scales=None, flags=0, stream=None) -> None:
+    """FC layers of a mixture of experts on 4-bit codes: the rows of y belong to experts in order, group_rows[e] to expert e, and
+    y[r] = act(x[x_rows[r]] w[e]^T + bias[e]).  Rows behind the last group's stay as they are."""
+    if xq.dim() != 2 or wq.dim() != 3 or _mx4_bad(xq, xs) or _mx4_bad(wq, ws) or xq.shape[1] != wq.shape[2]:
+        raise ValueError("q8_mx4_linear_grouped: shape mismatch")
+    E, N, K, M = wq.shape[0], wq.shape[1], 2 * xq.shape[1], y.shape[0]
+    if group_rows.numel() != E or (bias is not None and bias.numel() != E * N) or (xq.shape[0] if x_rows is None else x_rows.numel()) != M:
+        raise ValueError("q8_mx4_linear_grouped: group_rows, bias or x_rows size mismatch")
+    y_type = _product_output(y, y_scales, M, N, "q8_mx4_linear_grouped")
+    _ck(_binding.q8_mx4_linear_grouped(xq, xs, xq.shape[0], x_rows, wq, ws, bias, group_rows, E, M, N, K, y, y_type, y_scales, flags, _stream(stream)),
+        "q8_mx4_linear_grouped")
+
+
+def q8_linear_grouped(xq, wq, bias, sx, sw, group_rows, y, x_rows=None, out_amax=None, next_scale=None, flags=0, stream=None) -> None:
+    """FC layers of a mixture of experts on int8 codes: each expert's rows as q8_linear has them, with its own weights, scale and bias."""
+    if xq.dim() != 2 or wq.dim() != 3 or xq.shape[1] != wq.shape[2]:
+        raise ValueError("q8_linear_grouped: shape mismatch")
+    (E, N, K), M = wq.shape, y.shape[0]
+    if tuple(y.shape) != (M, N) or y.dtype != (torch.int8 if flags & EPI_REQUANT else torch.float32):
+        raise ValueError("q8_linear_grouped: y is [rows, N], fp32, or int8 with EPI_REQUANT")
+    if group_rows.numel() != E or sw.numel() != E or (bias is not None and bias.numel() != E * N) or (xq.shape[0] if x_rows is None else x_rows.numel()) != M:
+        raise ValueError("q8_linear_grouped: group_rows, scale, bias or x_rows size mismatch")
+    _ck(_binding.q8_linear_grouped(xq, xq.shape[0], x_rows, wq, bias, sx, sw, group_rows, E, M, N, K, y, out_amax, next_scale, flags,
+                                   _stream(stream)), "q8_linear_grouped")
+
+
+def q8_route(logits, experts, gates, group_rows, rows, slots, work, stream=None) -> None:
+    """The k = experts.shape[1] experts of each token by logit, their softmax, and the (token, choice) pairs sorted by expert:
+    group_rows and rows for the grouped products, slots for q8_combine."""
+    (T, E), k = logits.shape, experts.shape[1]
+    if tuple(experts.shape) != (T, k) or gates.numel() != T * k or group_rows.numel() != E or rows.numel() != T * k or slots.numel() != T * k:
+        raise ValueError("q8_route: shape mismatch")
+    if work.numel() < ROUTE_BLOCKS * E:
+        raise ValueError("q8_route: work holds ROUTE_BLOCKS * n_experts integers")
+    _ck(_binding.q8_route(logits, T, E, k, experts, gates, group_rows, rows, slots, work, _stream(stream)), "q8_route")
+
+
+def q8_combine(y, slots, gates, out, stream=None) -> None:
+    """out[t] = sum over j of gates[t, j] * y[slots[t, j]]."""
+    (T, k), (R, N) = slots.shape, y.shape
+    if gates.numel() != T * k or tuple(out.shape) != (T, N) or out.dtype != y.dtype:
+        raise ValueError("q8_combine: shape or type mismatch")
+    _ck(_binding.q8_combine(y, R, slots, gates, T, k, N, out, _float_type(y, "q8_combine"), _stream(stream)), "q8_combine")
 
 
 def raw():

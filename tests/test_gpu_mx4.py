@@ -1,0 +1,490 @@
+"""4-bit microscaled quantizers, FC layers on their codes, grouped products, router and combination on the GPU against their
+64-bit forms.  Tolerances by arithmetic:
+
+  codes and scales    equal (the quotient by a power of two and its rounding are exact), the sign of a zero aside
+  fp32 products       the terms are exact; a sum of K of them in fp32 passes through at most K / 64 matrix instructions, 8 partial sums
+                      and a bias, each of which may be off by 2^-23 of the magnitudes summed (a sum inside an instruction may be truncated):
+                      (K / 64 + 10) 2^-23 sum |x w|
+  GELU                its slope is at most 1.13, its own error 5.2e-7 and a rounding
+  bf16 outputs        half a step more: 2^-8 of the value
+"""
+import numpy as np
+import pytest
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+from oracle import mx4_oracle as MX  # noqa: E402
+
+
+@pytest.fixture(scope="module")
+def q8():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    from paper_1910_06188_amd import q8 as mod
+    return mod
+
+
+def dev(a):
+    return torch.from_numpy(np.ascontiguousarray(a)).cuda()
+
+
+def host(t):
+    return t.float().cpu().numpy().astype(np.float64) if t.is_floating_point() else t.cpu().numpy()
+
+
+TYPES = {"f32": torch.float32, "bf16": torch.bfloat16}
+
+
+def tensor(g, M, K, spread=2.0):
+    """Normal numbers whose rows and blocks lie orders of magnitude apart."""
+    x = g.standard_normal((M, K)) * np.exp(spread * g.standard_normal((M, 1))) * np.exp(g.standard_normal((1, K)))
+    return x.astype(np.float32)
+
+
+def same_codes(codes, want):
+    """Nibbles equal but for the sign of a zero."""
+    for a, b in ((codes & 15, want & 15), (codes >> 4, want >> 4)):
+        np.testing.assert_array_equal(np.where(a == 8, 0, a), np.where(b == 8, 0, b))
+
+
+def quantized(q8, x):
+    codes, scales = q8.mx4_empty(*x.shape)
+    codes.fill_(0xA5), scales.fill_(0x5A)
+    q8.q8_mx4_quantize(x, codes, scales)
+    return codes, scales
+
+
+# ---- quantizers ----------------------------------------------------------------------------------------------------------
+
+SHAPES = [(1, 1), (1, 32), (3, 33), (16, 768), (17, 127), (5, 128), (33, 129), (64, 1000), (100, 1024), (257, 520), (2, 8192), (1000, 31)]
+
+
+@pytest.mark.parametrize("M,K", SHAPES)
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+def test_quantize(q8, M, K, kind):
+    x = dev(tensor(np.random.default_rng(M * 1000 + K), M, K)).to(TYPES[kind])
+    codes, scales = quantized(q8, x)
+    want_c, want_s = MX.quantize(host(x))
+    np.testing.assert_array_equal(host(scales), want_s)
+    same_codes(host(codes), want_c)
+    xq = torch.full_like(x, 7)
+    q8.q8_mx4_fake_quantize(x, xq)
+    np.testing.assert_array_equal(host(xq), MX.values(want_c, want_s, K))
+    q8.q8_mx4_fake_quantize(x, x)                    # in place
+    assert torch.equal(x, xq)
+
+
+def test_quantize_every_rounding(q8):
+    """All quotients of 12 bits below 8, both signs, at scales over the whole range, subnormal ones among them."""
+    v = np.arange(4096) / 512.0
+    rows = []
+    for e in (-149, -130, -127, -126, -100, -3, 0, 1, 60, 124):
+        block = np.concatenate([v, -v]).reshape(-1, 16)
+        rows.append(np.concatenate([np.full((len(block), 1), 4.0), block, np.zeros((len(block), 15))], 1) * 2.0 ** e)
+    x = dev(np.concatenate(rows).astype(np.float32))
+    codes, scales = quantized(q8, x)
+    want_c, want_s = MX.quantize(host(x))
+    np.testing.assert_array_equal(host(scales), want_s)
+    same_codes(host(codes), want_c)
+    q8.q8_mx4_fake_quantize(x, x)
+    np.testing.assert_array_equal(host(x), MX.values(want_c, want_s, 32))
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+def test_quantize_infinities_and_nan(q8, kind):
+    g = np.random.default_rng(5)
+    x = tensor(g, 6, 200)
+    x[0, 3], x[1, 40], x[2, 199], x[3, 64] = np.inf, np.nan, -np.inf, -np.nan
+    x[4, 32:64], x[5, :] = 0, 0
+    x[4, 0] = float(np.finfo(np.float32).max) * 0.99
+    x = dev(x).to(TYPES[kind])
+    codes, scales = quantized(q8, x)
+    want_c, want_s = MX.quantize(host(x))
+    np.testing.assert_array_equal(host(scales), want_s)
+    same_codes(host(codes), want_c)
+    xq = torch.empty_like(x)
+    q8.q8_mx4_fake_quantize(x, xq)
+    np.testing.assert_array_equal(host(xq), MX.values(want_c, want_s, 200))     # NaN where the block is
+
+
+def test_quantize_rows_that_are_not_16_byte_aligned(q8):
+    flat = dev(tensor(np.random.default_rng(1), 1, 1 + 40 * 64))[0]
+    x = flat[1:].view(40, 64)                        # contiguous, four bytes past an aligned address
+    codes, scales = quantized(q8, x)
+    want_c, want_s = MX.quantize(host(x))
+    np.testing.assert_array_equal(host(scales), want_s)
+    same_codes(host(codes), want_c)
+
+
+def test_fake_quantize_gradient_is_straight_through(q8):
+    """The training step's pair: values of the codes forward; backward the gradient unchanged, which is the slope of the trend: over a
+    block whose scale does not move, the code's value moves with x by as much as x does, a step at a time."""
+    x = dev(tensor(np.random.default_rng(2), 8, 64))
+    grad, out = dev(tensor(np.random.default_rng(3), 8, 64)), torch.zeros(8, 64, device="cuda")
+    q8.q8_ste_backward(grad, out)
+    assert torch.equal(out, grad)
+    t = dev(np.repeat(np.arange(0, 4.0, 1 / 64, dtype=np.float32)[:, None], 32, 1))
+    t[:, 0] = 4.0                                     # fixes the scale of the block
+    q = torch.empty_like(t)
+    q8.q8_mx4_fake_quantize(t, q)
+    # between 0 and 4 the rounding is off by at most half a step of 1, so the mean slope over the range is 1 within 1 / 4
+    assert abs(float(q[-1, 5] - q[0, 5]) / float(t[-1, 5] - t[0, 5]) - 1) <= 0.25
+    assert float((q - t).abs().max()) <= 0.5
+
+
+# ---- products ------------------------------------------------------------------------------------------------------------
+
+def check_product(y, ref, mag, K, gelu, kind):
+    err = (K / 64 + 10) * 2.0 ** -23 * mag
+    if gelu:
+        ref, err = MX.gelu(ref), 1.13 * err + 5.2e-7 + 2.0 ** -23 * np.abs(ref)
+    if kind == "bf16":
+        err = err + 2.0 ** -8 * (np.abs(ref) + err)
+    off = np.abs(host(y) - ref)
+    assert (off <= err).all(), (float((off / np.maximum(err, 1e-300)).max()), np.unravel_index((off / np.maximum(err, 1e-300)).argmax(), off.shape))
+
+
+LINEARS = [(1, 1024, 4096), (1, 32, 1), (2, 1, 3), (3, 100, 33), (5, 129, 70), (16, 768, 768), (31, 384, 257), (32, 4096, 64), (33, 640, 96), (64, 256, 2000),
+           (129, 2100, 130), (300, 520, 300), (777, 1000, 520), (1500, 256, 384), (2048, 1024, 1024), (515, 4224, 644)]
+
+
+@pytest.mark.parametrize("M,K,N", LINEARS)
+@pytest.mark.parametrize("kind,gelu", [("f32", False), ("bf16", True)])
+def test_linear(q8, M, K, N, kind, gelu):
+    g = np.random.default_rng(M + K + N)
+    x, w, b = (dev(tensor(g, *s, spread=0.5)) for s in ((M, K), (N, K), (1, N)))
+    b = b.reshape(-1)
+    xq, wq = quantized(q8, x), quantized(q8, w)
+    flags = q8.EPI_GELU if gelu else 0
+    y = torch.full((M, N), 7, dtype=TYPES[kind], device="cuda")
+    q8.q8_mx4_linear(*xq, *wq, b, y, flags=flags)
+    xv, wv = (MX.values(host(c), host(s)) for c, s in (xq, wq))
+    ref, mag = MX.grouped(xv, [wv], [host(b)], [M], M)
+    check_product(y, ref, mag, K, gelu, kind)
+    dyn = torch.full_like(y, 7)
+    q8.q8_mx4_linear_dynamic(x, *wq, b, *q8.mx4_empty(M, K), dyn, flags=flags)
+    check_product(dyn, ref, mag, K, gelu, kind)
+    no_bias = torch.full_like(y, 7)
+    q8.q8_mx4_linear(*xq, *wq, None, no_bias, flags=flags)
+    ref, mag = MX.grouped(xv, [wv], None, [M], M)
+    check_product(no_bias, ref, mag, K, gelu, kind)
+
+
+@pytest.mark.parametrize("M,K,N", [(1, 1024, 4096), (7, 100, 128), (33, 768, 256), (300, 1000, 384), (1024, 512, 1024), (2500, 256, 2048)])
+@pytest.mark.parametrize("gelu", [False, True])
+def test_linear_to_codes(q8, M, K, N, gelu):
+    """4-bit outputs are the codes of the fp32 output, byte for byte."""
+    g = np.random.default_rng(M + K + N)
+    x, w, b = (dev(tensor(g, *s, spread=0.5)) for s in ((M, K), (N, K), (1, N)))
+    xq, wq = quantized(q8, x), quantized(q8, w)
+    flags = q8.EPI_GELU if gelu else 0
+    y = torch.empty((M, N), device="cuda")
+    q8.q8_mx4_linear(*xq, *wq, b, y, flags=flags)
+    want = quantized(q8, y)
+    codes, scales = q8.mx4_empty(M, N)
+    codes.fill_(0xA5), scales.fill_(0x5A)
+    q8.q8_mx4_linear(*xq, *wq, b, codes, y_scales=scales, flags=flags)
+    assert torch.equal(scales, want[1]) and torch.equal(codes, want[0])
+
+
+def test_linear_without_a_reduction_is_the_bias(q8):
+    b = torch.randn(70, device="cuda")
+    y = torch.empty((9, 70), device="cuda")
+    q8.q8_mx4_linear(*q8.mx4_empty(9, 0), *q8.mx4_empty(70, 0), b, y)
+    assert torch.equal(y, b.expand(9, 70))
+
+
+@pytest.mark.parametrize("M", [5, 600])
+def test_linear_follows_nan_and_infinity(q8, M):
+    g = np.random.default_rng(9)
+    x, w = tensor(g, M, 384, 0.3), tensor(g, 260, 384, 0.3)
+    x[2, 40], x[4, 383], w[7, 0], w[259, 200] = np.nan, np.inf, -np.inf, np.nan
+    y = torch.empty((M, 260), device="cuda")
+    q8.q8_mx4_linear(*quantized(q8, dev(x)), *quantized(q8, dev(w)), None, y)
+    bad = np.isnan(host(y))
+    want = np.zeros((M, 260), bool)
+    want[[2, 4]], want[:, [7, 259]] = True, True
+    np.testing.assert_array_equal(bad, want)
+
+
+# ---- grouped products ----------------------------------------------------------------------------------------------------
+
+GROUPS = [                                            # group_rows, rows of y, rows of x (None: no x_rows)
+    ([1], 1, None), ([3, 0, 5], 8, None), ([0, 0, 0, 2], 2, 7), ([40, 1, 0, 33, 64, 7], 145, 50), ([0, 0], 4, 9), ([-3, 5, -1, 100], 90, None),
+    ([2, 2], 9, 6), ([2 ** 31 - 1, 2 ** 31 - 1, 5], 40, 11), ([1] * 70 + [3] * 70, 280, 20), ([300, 500, 129, 0, 400], 1400, 300), ([0] * 200 + [130, 0, 260], 390, None),
+    ([1100, 1300], 2500, 900)]
+
+
+def routed_rows(g, M, n):
+    if n is None:
+        return None
+    rows = g.integers(0, n, M).astype(np.int32)
+    if M > 3:                                         # indices outside x count as rows of zeros
+        rows[1], rows[M // 2], rows[M - 1] = -1, n, 2 ** 31 - 1
+    return rows
+
+
+@pytest.mark.parametrize("group_rows,M,n", GROUPS)
+@pytest.mark.parametrize("K,N,kind,gelu", [(100, 70, "f32", False), (384, 256, "bf16", True), (1024, 384, "f32", True)])
+def test_mx4_grouped(q8, group_rows, M, n, K, N, kind, gelu):
+    g = np.random.default_rng(M + K)
+    E, rows = len(group_rows), routed_rows(g, M, n)
+    x, w = tensor(g, M if n is None else n, K, 0.5), tensor(g, E * N, K, 0.5)
+    b = g.standard_normal((E, N)).astype(np.float32)
+    xq = quantized(q8, dev(x))
+    per = [quantized(q8, dev(w[e * N: (e + 1) * N])) for e in range(E)]
+    wq = (torch.stack([c for c, _ in per]), torch.stack([s for _, s in per]))
+    y = torch.full((M, N), 7, dtype=TYPES[kind], device="cuda")
+    counts, x_rows = dev(np.array(group_rows, np.int32)), None if rows is None else dev(rows)
+    flags = q8.EPI_GELU if gelu else 0
+    q8.q8_mx4_linear_grouped(*xq, *wq, dev(b), counts, y, x_rows=x_rows, flags=flags)
+    ref, mag = MX.grouped(MX.values(host(xq[0]), host(xq[1])), [MX.values(host(c), host(s)) for c, s in per], b, group_rows, M, rows)
+    mine = ~np.isnan(ref[:, 0])
+    assert (host(y)[~mine] == 7).all()                # rows behind the last group's stay as they were
+    check_product(y[dev(mine)], ref[mine], mag[mine], K, gelu, kind)
+    if N % 128 == 0:
+        full, (codes, scales) = torch.zeros((M, N), device="cuda"), q8.mx4_empty(M, N)
+        q8.q8_mx4_linear_grouped(*xq, *wq, dev(b), counts, full, x_rows=x_rows, flags=flags)
+        want = quantized(q8, full)
+        codes.fill_(0xA5), scales.fill_(0x5A)
+        q8.q8_mx4_linear_grouped(*xq, *wq, dev(b), counts, codes, x_rows=x_rows, y_scales=scales, flags=flags)
+        keep = dev(mine)
+        assert torch.equal(codes[keep], want[0][keep]) and torch.equal(scales[:, keep], want[1][:, keep])
+        assert (codes[~keep] == 0xA5).all() and (scales[:, ~keep] == 0x5A).all()
+
+
+@pytest.mark.parametrize("group_rows,M,n", GROUPS)
+@pytest.mark.parametrize("K,N,flags", [(1, 3, 0), (100, 70, 1), (384, 256, 3), (1000, 130, 5), (1024, 384, 2)])
+def test_int8_grouped(q8, group_rows, M, n, K, N, flags):
+    """Each expert's rows bit for bit as q8_linear has them."""
+    g = np.random.default_rng(M + K)
+    E, rows = len(group_rows), routed_rows(g, M, n)
+    x = g.integers(-127, 128, (M if n is None else n, K)).astype(np.int8)
+    w = dev(g.integers(-127, 128, (E, N, K)).astype(np.int8))
+    b, sw = dev(g.standard_normal((E, N)).astype(np.float32)), dev((g.random(E) * 1000 + 500).astype(np.float32))
+    sx, ns = torch.tensor([31.7], device="cuda"), torch.tensor([40.0], device="cuda")
+    counts = dev(np.array(group_rows, np.int32))
+    dtype = torch.int8 if flags & q8.EPI_REQUANT else torch.float32
+    y, amax = torch.full((M, N), 7, dtype=dtype, device="cuda"), torch.zeros(1, device="cuda")
+    q8.q8_linear_grouped(dev(x), w, b, sx, sw, counts, y, x_rows=None if rows is None else dev(rows), out_amax=amax, next_scale=ns, flags=flags)
+    want, want_amax = torch.full_like(y, 7), torch.zeros(1, device="cuda")
+    mine = dev(MX.gathered(x, rows, M).astype(np.int8))
+    for e, (a, z) in enumerate(MX.spans(group_rows, M)):
+        if z > a:
+            q8.q8_linear(mine[a:z], w[e], b[e], sx, sw[e: e + 1], want[a:z], out_amax=want_amax, next_scale=ns, flags=flags)
+    assert torch.equal(y, want)
+    assert torch.equal(amax, want_amax)
+
+
+def test_int8_grouped_sums_in_64_bits(q8):
+    g = np.random.default_rng(4)
+    E, N, K, counts = 3, 200, 2064, [130, 0, 71]
+    x, w = g.integers(-127, 128, (201, K)).astype(np.int8), g.integers(-127, 128, (E, N, K)).astype(np.int8)
+    b, sw, sx = g.standard_normal((E, N)).astype(np.float32), np.array([900, 1000, 1100], np.float32), np.array([20.0], np.float32)
+    y = torch.empty((201, N), device="cuda")
+    q8.q8_linear_grouped(dev(x), dev(w), dev(b), dev(sx), dev(sw), dev(np.array(counts, np.int32)), y)
+    for e, (a, z) in enumerate(MX.spans(counts, 201)):
+        s = np.float32(sx[0] * sw[e])
+        v = (b[e] * s).astype(np.float32).astype(np.float64)
+        acc = x[a:z].astype(np.int64) @ w[e].astype(np.int64).T + (np.sign(v) * np.floor(np.abs(v) + 0.5)).astype(np.int64)
+        ref = acc / (float(sx[0]) * float(sw[e]))
+        # one rounding each of the sum to fp32, of the reciprocal and of their product
+        assert (np.abs(host(y)[a:z] - ref) <= 3 * 2.0 ** -24 * 1.001 * np.abs(ref)).all()
+
+
+@pytest.mark.parametrize("offset,K", [(1, 100), (4, 256), (8, 1040), (16, 1024)])
+def test_int8_grouped_any_alignment(q8, offset, K):
+    g = np.random.default_rng(offset)
+    N, counts = 300, [200, 313]
+    x, w = g.integers(-127, 128, (513, K)).astype(np.int8), g.integers(-127, 128, (2, N, K)).astype(np.int8)
+    fx, fw = torch.zeros(offset + x.size, dtype=torch.int8, device="cuda"), torch.zeros(offset + w.size, dtype=torch.int8, device="cuda")
+    fx[offset:], fw[offset:] = dev(x).view(-1), dev(w).view(-1)
+    sx, sw, n = torch.ones(1, device="cuda"), torch.ones(2, device="cuda"), dev(np.array(counts, np.int32))
+    a, b = torch.empty((513, N), device="cuda"), torch.empty((513, N), device="cuda")
+    q8.q8_linear_grouped(fx[offset:].view(513, K), fw[offset:].view(2, N, K), None, sx, sw, n, a)
+    q8.q8_linear_grouped(dev(x), dev(w), None, sx, sw, n, b)
+    assert torch.equal(a, b)
+    assert torch.equal(a[:200].double().cpu(), torch.from_numpy((x[:200].astype(np.int64) @ w[0].astype(np.int64).T).astype(np.float32)).double())
+
+
+# ---- router and combination ------------------------------------------------------------------------------------------------
+
+def check_route(q8, logits, k):
+    T, E = logits.shape
+    i32 = dict(dtype=torch.int32, device="cuda")
+    experts, rows, slots = (torch.full((T, k), -9, **i32) for _ in range(3))
+    gates, counts, work = torch.full((T, k), -9.0, device="cuda"), torch.full((E,), -9, **i32), torch.full((q8.ROUTE_BLOCKS * E,), -9, **i32)
+    q8.q8_route(dev(logits), experts, gates, counts, rows.view(-1), slots, work)
+    want = MX.route(logits, k)
+    for got, ref in zip((experts, counts, rows.view(-1), slots), (want[0], want[2], want[3], want[4])):
+        np.testing.assert_array_equal(host(got), ref)
+    # exp within 2^-22 (an argument of up to 100 rounded once and the function's own ulp or two), a sum of k, a division:
+    # an argument a is off by 2^-24 |a|, so exp(a) by that much of itself
+    lo = np.where(np.isneginf(logits) | np.isnan(logits), np.nan, np.clip(logits.astype(np.float64), -3.4e38, 3.4e38))
+    spread = 0.0 if not T or np.isnan(lo).all() else float(np.nanmax(np.where(np.abs(lo) < 1e3, np.abs(lo), 0))) * 2
+    err = (spread * 2.0 ** -24 * 2 + 2.0 ** -21 + k * 2.0 ** -23) * want[1] + 1e-37
+    assert (np.abs(host(gates) - want[1]) <= err).all()
+    return experts, gates, counts, rows, slots
+
+
+@pytest.mark.parametrize("T", [0, 1, 2, 63, 64, 65, 300, 3000])
+@pytest.mark.parametrize("E,k", [(1, 1), (3, 3), (8, 2), (64, 2), (65, 4), (128, 8), (200, 6), (257, 1), (1024, 16)])
+def test_route(q8, T, E, k):
+    if T * E > 700000:
+        T = 700
+    g = np.random.default_rng(T + E)
+    check_route(q8, (np.round(g.standard_normal((T, E)) * 8) / 8).astype(np.float32), k)      # many ties
+
+
+def test_route_a_large_batch(q8):
+    g = np.random.default_rng(0)
+    check_route(q8, (g.standard_normal((30000, 8)) * 3).astype(np.float32), 2)
+
+
+@pytest.mark.parametrize("T", [5, 400])
+@pytest.mark.parametrize("E,k", [(6, 4), (70, 5)])
+def test_route_masked_infinite_and_nan_logits(q8, T, E, k):
+    g = np.random.default_rng(T)
+    l = g.standard_normal((T, E)).astype(np.float32)
+    l[g.random((T, E)) < 0.4] = -np.inf
+    l[0], l[1], l[2] = -np.inf, np.nan, np.finfo(np.float32).min
+    l[3, :2], l[4, 1] = np.inf, np.inf
+    l[4, 2], l[3, 5] = np.nan, np.finfo(np.float32).max
+    check_route(q8, l, k)
+    l[0] = np.where(np.arange(E) % 2, -0.0, 0.0)      # equal: the lowest indices
+    check_route(q8, l, k)
+
+
+def test_route_everything_to_one_expert(q8):
+    l = np.zeros((1000, 16), np.float32)
+    l[:, 11] = 5
+    check_route(q8, l, 1)
+    check_route(q8, l, 2)
+
+
+@pytest.mark.parametrize("T,k,N", [(1, 1, 1), (3, 2, 33), (64, 2, 1024), (129, 6, 200), (40, 16, 8), (1000, 3, 768)])
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+def test_combine(q8, T, k, N, kind):
+    g = np.random.default_rng(T + N)
+    R = T * k + 3
+    y, gates = dev(g.standard_normal((R, N)).astype(np.float32)).to(TYPES[kind]), g.random((T, k)).astype(np.float32)
+    slots = g.permutation(R)[: T * k].reshape(T, k).astype(np.int32)
+    if T > 1:
+        slots[0, 0], slots[-1, -1], slots[1, 0] = -1, R, slots[0, k - 1]          # outside: nothing; the same row twice
+    out = torch.full((T, N), 7, dtype=TYPES[kind], device="cuda")
+    q8.q8_combine(y, dev(slots), dev(gates), out)
+    ok = (slots >= 0) & (slots < R)
+    terms = np.where(ok[..., None], gates[..., None].astype(np.float64) * host(y)[np.where(ok, slots, 0)], 0)
+    ref, mag = terms.sum(1), np.abs(terms).sum(1)
+    err = k * 2.0 ** -24 * 1.001 * mag                 # k fused additions, each rounded once
+    if kind == "bf16":
+        err = err + 2.0 ** -8 * (np.abs(ref) + err)
+    assert (np.abs(host(out) - ref) <= err).all()
+
+
+def test_combine_without_rows_is_zero(q8):
+    out = torch.full((4, 40), 7.0, device="cuda")
+    q8.q8_combine(torch.empty((0, 40), device="cuda"), torch.zeros((4, 2), dtype=torch.int32, device="cuda"), torch.ones((4, 2), device="cuda"), out)
+    assert (out == 0).all()
+
+
+# ---- together --------------------------------------------------------------------------------------------------------------
+
+class Moe:
+    """A mixture of experts on 4-bit codes as a program runs it: route, quantize, first layer with GELU to codes, second layer, combine."""
+
+    def __init__(self, q8, T, E, k, H, F, room=0, seed=0):
+        g = np.random.default_rng(seed)
+        self.q8, self.sizes = q8, (T, E, k, H, F)
+        self.x, self.logits = dev(tensor(g, T, H, 0.3)).bfloat16(), dev(g.standard_normal((T, E)).astype(np.float32))
+        self.w1, self.w2 = self.weights(g, E, F, H), self.weights(g, E, H, F)
+        self.b1, self.b2 = (dev((g.standard_normal((E, n)) * 0.1).astype(np.float32)) for n in (F, H))
+        i32 = dict(dtype=torch.int32, device="cuda")
+        R = T * k + room
+        self.experts, self.slots, self.counts = torch.empty((T, k), **i32), torch.empty((T, k), **i32), torch.empty(E, **i32)
+        self.rows, self.work, self.gates = torch.zeros(R, **i32), torch.empty(q8.ROUTE_BLOCKS * E, **i32), torch.empty((T, k), device="cuda")
+        self.xq, self.h = q8.mx4_empty(T, H), q8.mx4_empty(R, F)
+        self.h[0].zero_(), self.h[1].zero_()
+        self.y, self.out = torch.zeros((R, H), dtype=torch.bfloat16, device="cuda"), torch.zeros((T, H), dtype=torch.bfloat16, device="cuda")
+
+    def weights(self, g, E, N, K):
+        per = [quantized(self.q8, dev((g.standard_normal((N, K)) * K ** -0.5).astype(np.float32))) for _ in range(E)]
+        return torch.stack([c for c, _ in per]), torch.stack([s for _, s in per])
+
+    def run(self, stream=None):
+        q8, (T, E, k, H, F) = self.q8, self.sizes
+        q8.q8_route(self.logits, self.experts, self.gates, self.counts, self.rows[: T * k], self.slots, self.work, stream=stream)
+        q8.q8_mx4_quantize(self.x, *self.xq, stream=stream)
+        q8.q8_mx4_linear_grouped(*self.xq, *self.w1, self.b1, self.counts, self.h[0], x_rows=self.rows, y_scales=self.h[1], flags=q8.EPI_GELU, stream=stream)
+        q8.q8_mx4_linear_grouped(*self.h, *self.w2, self.b2, self.counts, self.y, stream=stream)
+        q8.q8_combine(self.y, self.slots, self.gates, self.out, stream=stream)
+        return self.out
+
+    def reference(self):
+        T, E, k, H, F = self.sizes
+        experts, gates, counts, rows, slots = MX.route(host(self.logits).astype(np.float32), k)
+        xv = MX.values(*MX.quantize(host(self.x)), H)
+        vals = lambda w, e, K: MX.values(host(w[0][e]), host(w[1][e]), K)  # noqa: E731
+        h, _ = MX.grouped(xv, [vals(self.w1, e, H) for e in range(E)], host(self.b1), counts, T * k, rows)
+        hv = MX.values(*MX.quantize(MX.gelu(h).astype(np.float32)), F)
+        y, _ = MX.grouped(hv, [vals(self.w2, e, F) for e in range(E)], host(self.b2), counts, T * k)
+        return (gates[..., None] * y[slots]).sum(1)
+
+
+@pytest.mark.parametrize("T,E,k,H,F,room", [(1, 4, 2, 128, 256, 0), (33, 8, 2, 200, 384, 5), (700, 6, 3, 256, 512, 40), (3000, 2, 1, 256, 256, 0)])
+def test_mixture_of_experts(q8, T, E, k, H, F, room):
+    m = Moe(q8, T, E, k, H, F, room)
+    got, ref = host(m.run()), m.reference()
+    # y and the sum are each rounded to bf16 (2^-8 each of values up to the largest); a code of the hidden layer that lies on a
+    # rounding border may fall on either side, which moves an output by a code's step times a weight: of F of them one or two
+    scale = np.abs(ref).max()
+    assert np.abs(got - ref).max() <= 3 * 2.0 ** -8 * scale + 0.02 * scale
+    assert np.linalg.norm(got - ref) <= 2.0 ** -7 * np.linalg.norm(ref)
+
+
+def test_mixture_of_experts_captured_and_replayed(q8):
+    m = Moe(q8, 150, 8, 2, 256, 512, room=10)
+    m.run()
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=s):
+        m.run()
+    for i in range(5):
+        m.logits.copy_(dev(np.random.default_rng(i).standard_normal((150, 8)).astype(np.float32)))
+        m.x.copy_(dev(tensor(np.random.default_rng(50 + i), 150, 256, 0.3)))
+        want = m.run().clone()
+        torch.cuda.synchronize()
+        m.out.zero_(), m.counts.zero_(), m.work.fill_(3)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(m.out, want), i
+
+
+def test_two_streams_at_once(q8):
+    """Two layers with buffers of their own on two streams give what each gives alone."""
+    a, b = Moe(q8, 90, 8, 2, 256, 512, seed=1), Moe(q8, 400, 4, 2, 256, 512, seed=2)
+    want = a.run().clone(), b.run().clone()
+    s, t = torch.cuda.Stream(), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for _ in range(4):
+        a.out.zero_(), b.out.zero_()
+        torch.cuda.synchronize()
+        a.run(stream=s), b.run(stream=t)
+        torch.cuda.synchronize()
+        assert torch.equal(a.out, want[0]) and torch.equal(b.out, want[1])
+
+
+def test_wrong_types_are_refused(q8):
+    x = torch.zeros((4, 128), device="cuda")
+    c, s = q8.mx4_empty(4, 128)
+    with pytest.raises(TypeError):
+        q8.q8_mx4_quantize(x, c.view(torch.int8), s)
+    n = torch.zeros(2, dtype=torch.int64, device="cuda")
+    with pytest.raises(TypeError):
+        q8.q8_mx4_linear_grouped(c, s, *q8.mx4_empty(2, 128, 128), None, n, x)
+    with pytest.raises(ValueError):
+        q8.q8_mx4_quantize(x.t().contiguous().t(), c, s)      # not contiguous
+    with pytest.raises(q8.Q8Error):
+        q8.q8_mx4_linear(c, s, *q8.mx4_empty(128, 128), None, x, flags=q8.EPI_REQUANT)
