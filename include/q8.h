@@ -436,7 +436,7 @@ q8_status q8_mx4_linear_dynamic(const void* x, int x_type, const uint8_t* wq, co
  *   the batch), and so do their scales where y holds 4-bit codes.
  *   y, y_type, y_scales, flags as q8_mx4_linear.  1 <= n_experts <= Q8_MAX_EXPERTS; M * N <= 2^34.
  */
-#define Q8_MAX_EXPERTS 65536
+#define Q8_MAX_EXPERTS 1024
 q8_status q8_mx4_linear_grouped(const uint8_t* xq, const uint8_t* xs, int64_t x_count, const int32_t* x_rows, const uint8_t* wq,
                                 const uint8_t* ws, const float* bias, const int32_t* group_rows, int n_experts, int64_t M, int64_t N,
                                 int64_t K, void* y, int y_type, uint8_t* y_scales, uint32_t flags, void* stream);
@@ -489,6 +489,13 @@ q8_status q8_combine(const void* y, int64_t R, const int32_t* slots, const float
  * while no other thread is inside q8_linear.  An unknown variant makes q8_linear return Q8_ERR_LAUNCH.
  */
 void q8_debug_set_gemm_variant(int variant);
+
+/*
+ * Forces the kernel behind the 4-bit and grouped products for every later call of this process: 0 = automatic choice (the default),
+ * 1 = the 32x32 tiles that take any size and alignment, 2 and up = one tile shape of the staged kernel (what it cannot take goes to 1).
+ * An unknown variant makes the products return Q8_ERR_LAUNCH.  Process-global and unsynchronised.
+ */
+void q8_debug_set_product_variant(int variant);
 
 /*
  * The dynamic quantizer (q8_quantize_dynamic, q8_linear_f32, q8_linear_f32_static) takes a one-pass kernel for

@@ -603,6 +603,8 @@ q8_status q8_debug_stream_copy(const void* src, void* dst, int64_t nbytes, void*
 /* Tuning hook for the benchmark (not part of the method): pick the MFMA tile variant, 0 = automatic. */
 void q8_debug_set_gemm_variant(int v) { q8::set_gemm_variant(v); }
 
+void q8_debug_set_product_variant(int v) { q8::set_product_variant(v); }
+
 void q8_debug_set_quantize_one_pass(int enabled, uint32_t barrier_polls)
 {
     q8::set_quantize_resident(enabled != 0, barrier_polls);

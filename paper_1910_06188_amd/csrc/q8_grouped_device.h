@@ -57,10 +57,28 @@ __device__ __forceinline__ unsigned wave_scan_most(unsigned v, unsigned most)
     return v;
 }
 
+// Rows are dealt out to groups in order and only as far as y goes, and a negative number of rows counts as none, so that whatever
+// group_rows holds no two groups share a row and none leaves y.  Every wave works this out by itself: the counts of 64 groups a pass, one
+// a lane, and two scans in the vector ALU.
+struct GroupPass {
+    unsigned start, upto;   // this lane's group: first row, first row behind it
+    unsigned tiles, ends;   // its tiles of kRows rows, and those of this pass up to its last
+};
+template <int kRows>
+__device__ __forceinline__ GroupPass group_pass(const int32_t* __restrict__ group_rows, int n_groups, unsigned M, int g0, unsigned before)
+{
+    const int lane = threadIdx.x & 63;
+    const unsigned n = g0 + lane < n_groups ? min((unsigned)max(group_rows[g0 + lane], 0), M) : 0u;
+    GroupPass q;
+    q.upto = min(before + wave_scan_most(n, M), M);
+    const unsigned prev = (unsigned)__shfl_up((int)q.upto, 1);
+    q.start = lane ? prev : before;
+    q.tiles = (q.upto - q.start + kRows - 1) / kRows;
+    q.ends = wave_scan_most(q.tiles, 0x7fffffffu);
+    return q;
+}
+
 // The t-th tile of kRows rows that stay inside a group: its group, its first row of y, its rows (0: there is no such tile).
-// Rows are dealt out in order and only as far as y goes, and a negative number of rows counts as none, so that whatever group_rows
-// holds no two groups share a row and none leaves y.  Every wave finds its tile by itself: the counts of 64 groups a pass, one a
-// lane, and two scans in the vector ALU.
 struct RowTile {
     int group, row, rows;
 };
@@ -71,25 +89,34 @@ __device__ __forceinline__ RowTile find_row_tile(const int32_t* __restrict__ gro
         const int row = (int)(t * kRows);
         return RowTile{0, row, min(kRows, M - row)};
     }
-    const int lane = threadIdx.x & 63;
     unsigned before = 0;  // rows of the groups already passed
     for (int g0 = 0; g0 < n_groups; g0 += 64) {
-        const int n = g0 + lane < n_groups ? min(max(group_rows[g0 + lane], 0), M) : 0;
-        const unsigned upto = min(before + wave_scan_most((unsigned)n, (unsigned)M), (unsigned)M);
-        const unsigned prev = (unsigned)__shfl_up((int)upto, 1);
-        const unsigned start = lane ? prev : before;
-        const unsigned tiles = (upto - start + kRows - 1) / kRows, ends = wave_scan_most(tiles, 0x7fffffffu);
-        const unsigned long long behind = __ballot(t < ends);
+        const GroupPass q = group_pass<kRows>(group_rows, n_groups, (unsigned)M, g0, before);
+        const unsigned long long behind = __ballot(t < q.ends);
         if (behind) {
             const int l = __builtin_ctzll(behind);
-            const unsigned first = (unsigned)__builtin_amdgcn_readlane((int)(ends - tiles), l);
-            const int row = __builtin_amdgcn_readlane((int)start, l) + (int)((t - first) * kRows);
-            return RowTile{g0 + l, row, min(kRows, __builtin_amdgcn_readlane((int)upto, l) - row)};
+            const unsigned first = (unsigned)__builtin_amdgcn_readlane((int)(q.ends - q.tiles), l);
+            const int row = __builtin_amdgcn_readlane((int)q.start, l) + (int)((t - first) * kRows);
+            return RowTile{g0 + l, row, min(kRows, __builtin_amdgcn_readlane((int)q.upto, l) - row)};
         }
-        t -= (unsigned)__builtin_amdgcn_readlane((int)ends, 63);
-        before = (unsigned)__builtin_amdgcn_readlane((int)upto, 63);
+        t -= (unsigned)__builtin_amdgcn_readlane((int)q.ends, 63);
+        before = (unsigned)__builtin_amdgcn_readlane((int)q.upto, 63);
     }
     return RowTile{0, 0, 0};
+}
+
+// How many such tiles there are.
+template <int kRows>
+__device__ __forceinline__ unsigned count_row_tiles(const int32_t* __restrict__ group_rows, int n_groups, int M)
+{
+    if (!group_rows) return (unsigned)(M + kRows - 1) / kRows;
+    unsigned before = 0, tiles = 0;
+    for (int g0 = 0; g0 < n_groups; g0 += 64) {
+        const GroupPass q = group_pass<kRows>(group_rows, n_groups, (unsigned)M, g0, before);
+        tiles += (unsigned)__builtin_amdgcn_readlane((int)q.ends, 63);
+        before = (unsigned)__builtin_amdgcn_readlane((int)q.upto, 63);
+    }
+    return tiles;
 }
 
 // Tiles of kRows rows that M rows in n_groups groups can have at most: every group that has rows may end inside a tile.

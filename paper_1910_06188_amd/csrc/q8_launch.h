@@ -90,6 +90,8 @@ struct Product {
     int y_type;                  // Q8_TYPE_*
     unsigned flags;
 };
+// set_product_variant: tuning hook, 0 = automatic.
+void set_product_variant(int v);
 int launch_product(bool mx4, const Product& p, hipStream_t st);
 // 32x32 tiles for any size and alignment (q8_grouped_direct.hip).
 int launch_product_direct(bool mx4, const Product& p, hipStream_t st);

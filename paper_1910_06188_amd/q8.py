@@ -89,6 +89,8 @@ _lib.q8_status_str.restype = C.c_char_p
 _lib.q8_status_str.argtypes = [C.c_int]
 _lib.q8_debug_set_gemm_variant.argtypes = [C.c_int]
 _lib.q8_debug_set_gemm_variant.restype = None
+_lib.q8_debug_set_product_variant.argtypes = [C.c_int]
+_lib.q8_debug_set_product_variant.restype = None
 _lib.q8_debug_set_quantize_one_pass.argtypes = [C.c_int, _u32]
 _lib.q8_debug_set_quantize_one_pass.restype = None
 
@@ -133,6 +135,11 @@ def status_str(code: int) -> str:
 
 def set_gemm_variant(v: int) -> None:
     _lib.q8_debug_set_gemm_variant(int(v))
+
+
+def set_product_variant(v: int) -> None:
+    """Tuning hook of the 4-bit and grouped products: one kernel for all of them (0: the automatic choice)."""
+    _lib.q8_debug_set_product_variant(int(v))
 
 
 def set_quantize_one_pass(enabled: bool = True, barrier_polls: int = 64) -> None:

@@ -133,6 +133,14 @@ def test_fake_quantize_gradient_is_straight_through(q8):
     assert float((q - t).abs().max()) <= 0.5
 
 
+# Every kernel behind the products on every shape (0: the automatic choice); what a variant cannot take goes to the first.
+@pytest.fixture(params=range(10), ids=lambda v: f"kernel{v}")
+def variant(q8, request):
+    q8.set_product_variant(request.param)
+    yield request.param
+    q8.set_product_variant(0)
+
+
 # ---- products ------------------------------------------------------------------------------------------------------------
 
 def check_product(y, ref, mag, K, gelu, kind):
@@ -151,7 +159,7 @@ LINEARS = [(1, 1024, 4096), (1, 32, 1), (2, 1, 3), (3, 100, 33), (5, 129, 70), (
 
 @pytest.mark.parametrize("M,K,N", LINEARS)
 @pytest.mark.parametrize("kind,gelu", [("f32", False), ("bf16", True)])
-def test_linear(q8, M, K, N, kind, gelu):
+def test_linear(q8, variant, M, K, N, kind, gelu):
     g = np.random.default_rng(M + K + N)
     x, w, b = (dev(tensor(g, *s, spread=0.5)) for s in ((M, K), (N, K), (1, N)))
     b = b.reshape(-1)
@@ -173,7 +181,7 @@ def test_linear(q8, M, K, N, kind, gelu):
 
 @pytest.mark.parametrize("M,K,N", [(1, 1024, 4096), (7, 100, 128), (33, 768, 256), (300, 1000, 384), (1024, 512, 1024), (2500, 256, 2048)])
 @pytest.mark.parametrize("gelu", [False, True])
-def test_linear_to_codes(q8, M, K, N, gelu):
+def test_linear_to_codes(q8, variant, M, K, N, gelu):
     """4-bit outputs are the codes of the fp32 output, byte for byte."""
     g = np.random.default_rng(M + K + N)
     x, w, b = (dev(tensor(g, *s, spread=0.5)) for s in ((M, K), (N, K), (1, N)))
@@ -188,7 +196,7 @@ def test_linear_to_codes(q8, M, K, N, gelu):
     assert torch.equal(scales, want[1]) and torch.equal(codes, want[0])
 
 
-def test_linear_without_a_reduction_is_the_bias(q8):
+def test_linear_without_a_reduction_is_the_bias(q8, variant):
     b = torch.randn(70, device="cuda")
     y = torch.empty((9, 70), device="cuda")
     q8.q8_mx4_linear(*q8.mx4_empty(9, 0), *q8.mx4_empty(70, 0), b, y)
@@ -196,7 +204,7 @@ def test_linear_without_a_reduction_is_the_bias(q8):
 
 
 @pytest.mark.parametrize("M", [5, 600])
-def test_linear_follows_nan_and_infinity(q8, M):
+def test_linear_follows_nan_and_infinity(q8, variant, M):
     g = np.random.default_rng(9)
     x, w = tensor(g, M, 384, 0.3), tensor(g, 260, 384, 0.3)
     x[2, 40], x[4, 383], w[7, 0], w[259, 200] = np.nan, np.inf, -np.inf, np.nan
@@ -227,7 +235,7 @@ def routed_rows(g, M, n):
 
 @pytest.mark.parametrize("group_rows,M,n", GROUPS)
 @pytest.mark.parametrize("K,N,kind,gelu", [(100, 70, "f32", False), (384, 256, "bf16", True), (1024, 384, "f32", True)])
-def test_mx4_grouped(q8, group_rows, M, n, K, N, kind, gelu):
+def test_mx4_grouped(q8, variant, group_rows, M, n, K, N, kind, gelu):
     g = np.random.default_rng(M + K)
     E, rows = len(group_rows), routed_rows(g, M, n)
     x, w = tensor(g, M if n is None else n, K, 0.5), tensor(g, E * N, K, 0.5)
@@ -256,7 +264,7 @@ def test_mx4_grouped(q8, group_rows, M, n, K, N, kind, gelu):
 
 @pytest.mark.parametrize("group_rows,M,n", GROUPS)
 @pytest.mark.parametrize("K,N,flags", [(1, 3, 0), (100, 70, 1), (384, 256, 3), (1000, 130, 5), (1024, 384, 2)])
-def test_int8_grouped(q8, group_rows, M, n, K, N, flags):
+def test_int8_grouped(q8, variant, group_rows, M, n, K, N, flags):
     """Each expert's rows bit for bit as q8_linear has them."""
     g = np.random.default_rng(M + K)
     E, rows = len(group_rows), routed_rows(g, M, n)
@@ -294,7 +302,7 @@ def test_int8_grouped_sums_in_64_bits(q8):
 
 
 @pytest.mark.parametrize("offset,K", [(1, 100), (4, 256), (8, 1040), (16, 1024)])
-def test_int8_grouped_any_alignment(q8, offset, K):
+def test_int8_grouped_any_alignment(q8, variant, offset, K):
     g = np.random.default_rng(offset)
     N, counts = 300, [200, 313]
     x, w = g.integers(-127, 128, (513, K)).astype(np.int8), g.integers(-127, 128, (2, N, K)).astype(np.int8)
@@ -460,6 +468,15 @@ def test_mixture_of_experts_captured_and_replayed(q8):
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(m.out, want), i
+
+
+def test_an_unknown_kernel_is_an_error(q8):
+    q8.set_product_variant(99)
+    try:
+        with pytest.raises(q8.Q8Error):
+            q8.q8_mx4_linear(*q8.mx4_empty(4, 128), *q8.mx4_empty(4, 128), None, torch.empty((4, 4), device="cuda"))
+    finally:
+        q8.set_product_variant(0)
 
 
 def test_two_streams_at_once(q8):

@@ -93,7 +93,7 @@ def test_products_refuse(lib):
         for bad in ({"y": x}, {"y": w + 64}, {"y": xs}, {"y": ws}, {"y": b}, {"t": MX4, "ys": x}, {"t": MX4, "ys": y + 64}):
             assert f(**bad) == OVERLAP, bad
         assert f(M=0, x=None, xs=None, w=None, ws=None, y=None) == OK and f(N=0) == OK
-    for bad in ({"E": 0}, {"E": 65537}, {"n": 3}, {"n": 0, "rows": r}, {"n": -1}, {"n": 1 << 31, "rows": r}):
+    for bad in ({"E": 0}, {"E": 1025}, {"n": 3}, {"n": 0, "rows": r}, {"n": -1}, {"n": 1 << 31, "rows": r}):
         assert grouped(**bad) == SHAPE, bad
     assert grouped(g=None) == NULL
     assert grouped(g=g + 2) == ALIGN and grouped(rows=r + 2) == ALIGN
@@ -114,7 +114,7 @@ def test_int8_grouped_refuses(lib):
     def f(M=4, N=8, K=16, n=4, E=2, x=x, rows=None, w=w, b=b, sx=sx, sw=sw, g=g, y=y, a=None, ns=None, flags=0):
         return lib.q8_linear_grouped(x, n, rows, w, b, sx, sw, g, E, M, N, K, y, a, ns, flags, None)
 
-    for bad in ({"M": -1}, {"N": -1}, {"K": -1}, {"K": 131072}, {"E": 0}, {"n": 5}, {"n": 0, "rows": r}, {"M": 1 << 31}, {"E": 65537}):
+    for bad in ({"M": -1}, {"N": -1}, {"K": -1}, {"K": 131072}, {"E": 0}, {"n": 5}, {"n": 0, "rows": r}, {"M": 1 << 31}, {"E": 1025}):
         assert f(**bad) == SHAPE, bad
     for bad in ({"flags": 8}, {"flags": 2}, {"flags": 4}):
         assert f(**bad) == FLAGS, bad
