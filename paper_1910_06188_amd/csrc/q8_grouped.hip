@@ -8,27 +8,27 @@
 
 namespace q8 {
 
-int launch_product_64x64_s2(bool, const Product&, hipStream_t);
-int launch_product_64x128_s2(bool, const Product&, hipStream_t);
-int launch_product_128x128_s1(bool, const Product&, hipStream_t);
-int launch_product_128x128_s2(bool, const Product&, hipStream_t);
+int launch_product_64x64_s1(bool, const Product&, hipStream_t);
+int launch_product_64x128_s1(bool, const Product&, hipStream_t);
+int launch_product_128x128_s1b(bool, const Product&, hipStream_t);
+int launch_product_128x128_s1w2(bool, const Product&, hipStream_t);
 int launch_product_256x128_s1(bool, const Product&, hipStream_t);
+int launch_product_256x128_w8(bool, const Product&, hipStream_t);
 int launch_product_256x256_s2(bool, const Product&, hipStream_t);
-int launch_product_256x256_s1(bool, const Product&, hipStream_t);
-int launch_product_64x256_s1(bool, const Product&, hipStream_t);
+int launch_product_256x256_w4(bool, const Product&, hipStream_t);
 
 static const struct {
     int (*launch)(bool, const Product&, hipStream_t);
     int rows;
 } kTiles[] = {
-    {launch_product_64x64_s2, 64},
-    {launch_product_64x128_s2, 64},
-    {launch_product_128x128_s1, 128},
-    {launch_product_128x128_s2, 128},
+    {launch_product_64x64_s1, 64},
+    {launch_product_64x128_s1, 64},
+    {launch_product_128x128_s1b, 128},
+    {launch_product_128x128_s1w2, 128},
     {launch_product_256x128_s1, 256},
+    {launch_product_256x128_w8, 256},
     {launch_product_256x256_s2, 256},
-    {launch_product_256x256_s1, 256},
-    {launch_product_64x256_s1, 64}};
+    {launch_product_256x256_w4, 256}};
 
 static int g_variant = 0;
 void set_product_variant(int v) { g_variant = v; }

@@ -148,6 +148,12 @@ __device__ __forceinline__ float product_value(typename Op::Sum sum, const Produ
         return (float)(sum + c.bq) * c.r;
 }
 
+template <class Op>
+__device__ __forceinline__ float product_gelu(float v)
+{
+    return Op::kMx4 ? gelu_erf_nan(v) : gelu_erf(v);
+}
+
 // Maximum over each half of 32 lanes.
 __device__ __forceinline__ unsigned half_wave_max_u32(unsigned v)
 {

@@ -137,7 +137,7 @@ __global__ __launch_bounds__(KW * 64, 4) void product_direct_kernel(Product p, u
 #pragma unroll
             for (int w = 1; w < KW; ++w) sum += part[(w * kPdTile + r) * kRow + l32];
             float y = product_value<Op>(sum, c);
-            if (gelu) y = gelu_erf(y);
+            if (gelu) y = product_gelu<Op>(y);
             const int64_t m = tile.row + r, at = m * p.N + n;
             if (p.y_type == Q8_TYPE_MX4) {
                 const unsigned byte = mx4_scale_byte(half_wave_max_u32(f32_abs_bits(y)));

@@ -21,13 +21,15 @@ __device__ __forceinline__ void lds_dma4(v4i rsrc, unsigned voff, unsigned lds_a
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds" : : "s"(lds_addr), "v"(voff), "s"(rsrc) : "memory");
 }
 
-// kOut: the type of y.  For 4-bit outputs the MFMA's operands change places, so that a lane holds one row and 16 columns of a 32x32
-// block, and a block of the format -- 32 neighbours of a row -- is two lanes'.
-template <class Op, int BM, int BN, int WGM, int WGN, int kSlots, int kWgs, int kOut>
+// The MFMA takes w as its first operand and x as its second, so that a lane holds one row of y and 16 columns of a 32x32 block, four
+// times four neighbours, and a block of the 4-bit format -- 32 neighbours of a row -- is two lanes', its largest magnitude one exchange away.
+// The bias is what the sums start from.
+//
+// kOut: the type of y.
+template <class Op, int BM, int BN, int WGM, int WGN, int kSlots, int kAhead, int kWgs, int kOut>
 __global__ __launch_bounds__(WGM* WGN * 64, kWgs* WGM* WGN / 4) void product_tile_kernel(Product p, unsigned tiles_n, unsigned group_m)
 {
 #if defined(__HIP_DEVICE_COMPILE__)
-    constexpr bool kSwap = kOut == Q8_TYPE_MX4;
     constexpr int NW = WGM * WGN;
     constexpr int TM = BM / WGM, TN = BN / WGN, FM = TM / 32, FN = TN / 32;
     constexpr int A_BYTES = BM * kBK, B_BYTES = BN * kBK, OPERANDS = A_BYTES + B_BYTES;
@@ -37,8 +39,10 @@ __global__ __launch_bounds__(WGM* WGN * 64, kWgs* WGM* WGN / 4) void product_til
     static_assert(BM % (8 * NW) == 0 && BN % (8 * NW) == 0, "tile rows must split over the waves");
     static_assert(TM % 32 == 0 && TN % 32 == 0 && BM % 64 == 0 && BN % 64 == 0, "whole MFMA blocks and whole scale loads");
     static_assert(kSlots == 1 || kSlots == 2, "the waits below are for all loads");
-    static_assert(kWgs * kSlots * SLOT <= 160 * 1024, "LDS is 160 KiB per compute unit");
+    static_assert(kWgs * (kSlots * SLOT + BN * 4) <= 160 * 1024, "LDS is 160 KiB per compute unit");
+    using Sum = typename Op::Sum;
     __shared__ __attribute__((aligned(1024))) char lds[kSlots * SLOT];
+    __shared__ __attribute__((aligned(16))) Sum first[BN];  // what the sums of each column start from
 
     const int lane = threadIdx.x & 63, l32 = lane & 31, hi = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -76,102 +80,97 @@ __global__ __launch_bounds__(WGM* WGN * 64, kWgs* WGM* WGN / 4) void product_til
         const int r = (wave * B_LOADS + i) * 8 + row8;
         b_off[i] = (unsigned)min(r, last_b) * (unsigned)pitch + (unsigned)((chunk ^ swizzle_of_row(r)) * 16);
     }
-    // The scale loads of this wave: which operand, which group of the stage, which 64 rows.
-    unsigned s_off[S_LOADS ? S_LOADS : 1];
+    // The scale loads of this wave, 64 rows of one group of a stage each: the words of its group in the first stage, from one stage to the
+    // next, and how far they go.
     const int groups = pitch / 64;
+    unsigned s_off[S_LOADS ? S_LOADS : 1];
+    const uint8_t* s_base[S_LOADS ? S_LOADS : 1];
+    int64_t s_step[S_LOADS ? S_LOADS : 1];
+    unsigned s_extent[S_LOADS ? S_LOADS : 1];
+    int s_group[S_LOADS ? S_LOADS : 1];
     if constexpr (Op::kMx4) {
 #pragma unroll
         for (int i = 0; i < S_LOADS; ++i) {
             const int u = wave + i * NW;
-            if (u < BM / 32) {
-                const int id = x_row(u % (BM / 64) * 64 + lane);
-                s_off[i] = id < 0 ? kOutOfRange : (unsigned)id * 4u;
-            } else {
-                s_off[i] = (unsigned)min((u - BM / 32) % (BN / 64) * 64 + lane, last_b) * 4u;
-            }
+            const bool of_x = u < BM / 32;
+            const int v = of_x ? u : u - BM / 32, per = of_x ? BM / 64 : BN / 64;
+            const int r = v % per * 64 + lane, id = of_x ? x_row(r) : min(r, last_b);
+            s_off[i] = id < 0 ? kOutOfRange : (unsigned)id * 4u;
+            s_group[i] = v / per;
+            const int64_t rows = of_x ? p.x_count : (int64_t)N;
+            const uint8_t* all = of_x ? p.xs + x_first * 4 : p.ws + ((int64_t)tile.group * groups * N + n0) * 4;
+            s_base[i] = all + s_group[i] * rows * 4;
+            s_step[i] = rows * 8;
+            s_extent[i] = (of_x ? x_extent : (unsigned)(last_b + 1)) * 4u;
         }
     }
 
-    const int KT = (pitch + kBK - 1) / kBK;
-    const v4i qa = make_rsrc(Xt, x_extent * (unsigned)pitch), qb = make_rsrc(Wt, (unsigned)(last_b + 1) * (unsigned)pitch);
-    auto load_stage = [&](int kt, int slot) {
+    const int KT = pitch / kBK, tail = pitch % kBK;  // whole stages, and the bytes behind them (a whole number of 16)
+    const unsigned extent_a = x_extent * (unsigned)pitch, extent_b = (unsigned)(last_b + 1) * (unsigned)pitch;
+    // Stage kt into a slot; past the end of the rows through empty descriptors, which fetch nothing.
+    auto load_stage = [&](int kt, int slot, auto whole) {
+        constexpr bool kWhole = decltype(whole)::value;
         const unsigned koff = (unsigned)kt * kBK, dst = lds_base + (unsigned)(slot * SLOT);
-        const int left = pitch - kt * kBK;  // bytes of the rows from this stage on
-        if (left >= kBK) {
+        const bool live = !kWhole || kt < KT;
+        const v4i qa = make_rsrc(Xt, live ? extent_a : 0u), qb = make_rsrc(Wt, live ? extent_b : 0u);
+        auto at = [&](unsigned off, int r) { return kWhole || ((chunk ^ swizzle_of_row(r)) * 16 < tail) ? off : kOutOfRange; };
 #pragma unroll
-            for (int i = 0; i < A_LOADS; ++i) lds_dma16_first(qa, a_off[i], koff, dst + (wave * A_LOADS + i) * 1024);
+        for (int i = 0; i < A_LOADS; ++i)
+            lds_dma16_first(qa, at(a_off[i], (wave * A_LOADS + i) * 8 + row8), koff, dst + (wave * A_LOADS + i) * 1024);
 #pragma unroll
-            for (int i = 0; i < B_LOADS; ++i) lds_dma16_first(qb, b_off[i], koff, dst + A_BYTES + (wave * B_LOADS + i) * 1024);
-        } else {  // rows end inside the stage (after a whole number of 16 bytes)
-#pragma unroll
-            for (int i = 0; i < A_LOADS; ++i) {
-                const int c = (chunk ^ swizzle_of_row((wave * A_LOADS + i) * 8 + row8)) * 16;
-                lds_dma16_first(qa, c < left ? a_off[i] : kOutOfRange, koff, dst + (wave * A_LOADS + i) * 1024);
-            }
-#pragma unroll
-            for (int i = 0; i < B_LOADS; ++i) {
-                const int c = (chunk ^ swizzle_of_row((wave * B_LOADS + i) * 8 + row8)) * 16;
-                lds_dma16_first(qb, c < left ? b_off[i] : kOutOfRange, koff, dst + A_BYTES + (wave * B_LOADS + i) * 1024);
-            }
-        }
+        for (int i = 0; i < B_LOADS; ++i)
+            lds_dma16_first(qb, at(b_off[i], (wave * B_LOADS + i) * 8 + row8), koff, dst + A_BYTES + (wave * B_LOADS + i) * 1024);
         if constexpr (Op::kMx4) {
 #pragma unroll
             for (int i = 0; i < S_LOADS; ++i) {
                 const int u = wave + i * NW;
-                if (u < BM / 32) {
-                    const int g = 2 * kt + u / (BM / 64);
-                    lds_dma4(make_rsrc(p.xs + ((int64_t)g * p.x_count + x_first) * 4, g < groups ? x_extent * 4u : 0u), s_off[i], dst + OPERANDS + u * 256);
-                } else if (u < S_UNITS) {
-                    const int g = 2 * kt + (u - BM / 32) / (BN / 64);
-                    lds_dma4(make_rsrc(p.ws + (((int64_t)tile.group * groups + g) * N + n0) * 4, g < groups ? (unsigned)(last_b + 1) * 4u : 0u), s_off[i],
-                             dst + OPERANDS + u * 256);
-                }
+                if (S_UNITS % NW == 0 || u < S_UNITS) lds_dma4(make_rsrc(s_base[i], live && (kWhole || s_group[i] == 0) ? s_extent[i] : 0u), s_off[i], dst + OPERANDS + u * 256);
+                s_base[i] += live ? s_step[i] : 0;
             }
         }
     };
 
     const int wm = wave / WGN, wn = wave % WGN;
-    int a_row[FM], b_row[FN], a_sw[FM], b_sw[FN];
+    // Where this lane finds its 16 bytes of step ks in the first block of its wave's rows.  32 rows on, a row's swizzle differs in bit 2 alone,
+    // so the block behind is 4 KiB away and the chunk's bit flipped: the blocks need no addresses of their own.
+    static_assert((TM == 32 || TM % 64 == 0) && (TN == 32 || TN % 64 == 0), "the swizzles of a wave's blocks");
+    int a_lane[kKS], b_lane[kKS];
 #pragma unroll
-    for (int f = 0; f < FM; ++f) {
-        const int r = wm * TM + f * 32 + l32;
-        a_row[f] = r * kBK;
-        a_sw[f] = swizzle_of_row(r);
-    }
-#pragma unroll
-    for (int f = 0; f < FN; ++f) {
-        const int r = wn * TN + f * 32 + l32;
-        b_row[f] = A_BYTES + r * kBK;
-        b_sw[f] = swizzle_of_row(r);
+    for (int ks = 0; ks < kKS; ++ks) {
+        const int ra = wm * TM + l32, rb = wn * TN + l32;
+        a_lane[ks] = ra * kBK + (((4 * hi + ks) ^ swizzle_of_row(ra)) << 4);
+        b_lane[ks] = A_BYTES + rb * kBK + (((4 * hi + ks) ^ swizzle_of_row(rb)) << 4);
     }
     const int a_sc = OPERANDS + (hi * BM + wm * TM + l32) * 4, b_sc = OPERANDS + BM * 8 + (hi * BN + wn * TN + l32) * 4;
 
+    load_stage(0, 0, std::true_type{});
+    const float sx = Op::kMx4 ? 0.0f : p.sx[0];
+    for (int t = threadIdx.x; t < BN; t += NW * 64) {
+        const ProductColumn c = product_column<Op>(p, tile.group, min(n0 + t, N - 1), sx);
+        if constexpr (Op::kMx4)
+            first[t] = c.b;
+        else
+            first[t] = c.bq;
+    }
+    __builtin_amdgcn_s_waitcnt(waitcnt_vm_lgkm0(0));
+    __syncthreads();
+
+    // Accumulator register e of lane l is column 8 (e / 4) + 4 (l / 32) + e % 4 and row l % 32 of its block.
+    typedef Sum v4s __attribute__((ext_vector_type(4)));
     typename Op::Acc acc[FM][FN];
 #pragma unroll
-    for (int i = 0; i < FM; ++i)
+    for (int j = 0; j < FN; ++j)
 #pragma unroll
-        for (int j = 0; j < FN; ++j)
+        for (int q = 0; q < 4; ++q) {
+            const v4s c = *reinterpret_cast<const v4s*>(first + wn * TN + j * 32 + 8 * q + 4 * hi);
 #pragma unroll
-            for (int e = 0; e < 16; ++e) acc[i][j][e] = 0;
-
-    if constexpr (kSlots == 2)
-        if (KT) load_stage(0, 0);
-    for (int kt = 0; kt < KT; ++kt) {
-        if constexpr (kSlots == 1) {
-            if (kt) {  // every wave has read the last stage
-                __builtin_amdgcn_s_waitcnt(waitcnt_vm_lgkm0(63));
-                __syncthreads();
-            }
-            load_stage(kt, 0);
-            __builtin_amdgcn_s_waitcnt(waitcnt_vm_lgkm0(0));
-            __syncthreads();
-        } else {
-            // own loads of stage kt have landed, own reads of stage kt - 1 are complete; its slot is free behind the barrier
-            __builtin_amdgcn_s_waitcnt(waitcnt_vm_lgkm0(0));
-            __syncthreads();
-            if (kt + 1 < KT) load_stage(kt + 1, (kt + 1) & 1);
+            for (int i = 0; i < FM; ++i)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) acc[i][j][4 * q + e] = c[e];
         }
-        const char* stage = lds + (kSlots == 2 ? (kt & 1) * SLOT : 0);
+
+    // The MFMAs of a stage.  The fragments come kAhead - 1 steps ahead of them; as soon as the last are under way, `loads` may ask for the next stage.
+    auto multiply = [&](const char* stage, auto loads) {
         int sa[FM], sb[FN];
         if constexpr (Op::kMx4) {
 #pragma unroll
@@ -179,132 +178,211 @@ __global__ __launch_bounds__(WGM* WGN * 64, kWgs* WGM* WGN / 4) void product_til
 #pragma unroll
             for (int f = 0; f < FN; ++f) sb[f] = *reinterpret_cast<const int*>(stage + b_sc + f * 128);
         }
-        v4i fa[2][FM], fb[2][FN];
+        v4i fa[kAhead][FM], fb[kAhead][FN];
         auto read_step = [&](int ks) {
 #pragma unroll
-            for (int f = 0; f < FM; ++f) fa[ks & 1][f] = *reinterpret_cast<const v4i*>(stage + a_row[f] + (((4 * hi + ks) ^ a_sw[f]) << 4));
+            for (int f = 0; f < FM; ++f) fa[ks % kAhead][f] = *reinterpret_cast<const v4i*>(stage + (a_lane[ks] ^ ((f & 1) << 6)) + f * 32 * kBK);
 #pragma unroll
-            for (int f = 0; f < FN; ++f) fb[ks & 1][f] = *reinterpret_cast<const v4i*>(stage + b_row[f] + (((4 * hi + ks) ^ b_sw[f]) << 4));
+            for (int f = 0; f < FN; ++f) fb[ks % kAhead][f] = *reinterpret_cast<const v4i*>(stage + (b_lane[ks] ^ ((f & 1) << 6)) + f * 32 * kBK);
         };
-        read_step(0);
+#pragma unroll
+        for (int ks = 0; ks < kAhead - 1; ++ks) read_step(ks);
         static_for<0, kKS>([&](auto kc) {
-            constexpr int ks = decltype(kc)::value;
-            if constexpr (ks + 1 < kKS) read_step(ks + 1);
+            constexpr int ks = decltype(kc)::value, next = ks + kAhead - 1;
+            if constexpr (next < kKS) read_step(next);
+            if constexpr (next == kKS - 1) {
+                __builtin_amdgcn_sched_barrier(0);
+                loads();
+                __builtin_amdgcn_sched_barrier(0);
+            }
 #pragma unroll
             for (int i = 0; i < FM; ++i)
 #pragma unroll
-                for (int j = 0; j < FN; ++j) {
-                    if constexpr (kSwap)
-                        acc[i][j] = Op::template mfma<ks>(fb[ks & 1][j], fa[ks & 1][i], acc[i][j], Op::kMx4 ? sb[j] : 0, Op::kMx4 ? sa[i] : 0);
-                    else
-                        acc[i][j] = Op::template mfma<ks>(fa[ks & 1][i], fb[ks & 1][j], acc[i][j], Op::kMx4 ? sa[i] : 0, Op::kMx4 ? sb[j] : 0);
-                }
+                for (int j = 0; j < FN; ++j)
+                    acc[i][j] = Op::template mfma<ks>(fb[ks % kAhead][j], fa[ks % kAhead][i], acc[i][j], Op::kMx4 ? sb[j] : 0, Op::kMx4 ? sa[i] : 0);
+            __builtin_amdgcn_sched_barrier(0);  // fragments of later steps would only take registers
         });
+    };
+    // One slot: the next stage loads as soon as every wave holds the last fragments of this one, under the MFMAs that are left.  Two: into the
+    // other slot from the start.
+    for (int kt = 0; kt < KT; ++kt) {
+        if constexpr (kSlots == 2) load_stage(kt + 1, (kt + 1) & 1, std::true_type{});
+        multiply(lds + (kSlots == 2 ? (kt & 1) * SLOT : 0), [&] {
+            if constexpr (kSlots == 1) {
+                __builtin_amdgcn_s_waitcnt(waitcnt_vm_lgkm0(63));
+                __syncthreads();
+                load_stage(kt + 1, 0, std::true_type{});
+            }
+        });
+        __builtin_amdgcn_s_waitcnt(waitcnt_vm_lgkm0(0));  // own loads have landed and own reads are complete
+        __syncthreads();
+    }
+    if (tail) {
+        load_stage(KT, 0, std::false_type{});
+        __builtin_amdgcn_s_waitcnt(waitcnt_vm_lgkm0(0));
+        __syncthreads();
+        multiply(lds, [] {});
     }
 
-    // Epilogue.  Accumulator register e of lane l is row 8 (e / 4) + 4 (l / 32) + e % 4 and column l % 32 of its block (kSwap: the other way round).
+    // Epilogue.
+    typedef unsigned v2u __attribute__((ext_vector_type(2)));
+    typedef unsigned v4u __attribute__((ext_vector_type(4)));
     const bool gelu = p.flags & Q8_EPI_GELU;
     constexpr int kSize = kOut == Q8_TYPE_F32 ? 4 : kOut == Q8_TYPE_BF16 ? 2 : 1;
-    if constexpr (kSwap) {
-        const int row_bytes = N / 2;
-        const __amdgpu_buffer_rsrc_t ry = __builtin_amdgcn_make_buffer_rsrc(static_cast<char*>(p.y) + (int64_t)tile.row * row_bytes, 0, tile.rows * row_bytes, 0x00020000);
-        const float* bias = p.bias ? p.bias + (int64_t)tile.group * N : nullptr;
+    const int row_bytes = kOut == Q8_TYPE_MX4 ? N / 2 : N * kSize;
+    const __amdgpu_buffer_rsrc_t ry = __builtin_amdgcn_make_buffer_rsrc(static_cast<char*>(p.y) + (int64_t)tile.row * row_bytes, 0, tile.rows * row_bytes, 0x00020000);
+    const float r = Op::kMx4 ? 1.0f : dequant_factor(sx, p.sw[tile.group]);
+    const float next_scale = kOut == Q8_TYPE_I8 ? p.next_scale[0] : 0.0f;
+    float famax = 0.0f;
+    // Block (i, j) as fp32 values: row l32, columns 8 (e / 4) + 4 hi + e % 4.
+    auto block_values = [&](int i, int j, float* v) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+            if constexpr (Op::kMx4)
+                v[e] = acc[i][j][e];
+            else
+                v[e] = (float)acc[i][j][e] * r;
+        }
+        if (gelu) {
+#pragma unroll
+            for (int e = 0; e < 16; ++e) v[e] = product_gelu<Op>(v[e]);
+        }
+        if constexpr (!Op::kMx4) {
+            if (p.flags & Q8_EPI_ABSMAX) {
+                float a = 0.0f;
+#pragma unroll
+                for (int e = 0; e < 16; ++e)
+                    if (n0 + wn * TN + j * 32 + 8 * (e >> 2) + 4 * hi + (e & 3) < N) a = __builtin_fmaxf(a, __builtin_fabsf(v[e]));
+                if (wm * TM + i * 32 + l32 < tile.rows) famax = __builtin_fmaxf(famax, a);
+            }
+        }
+    };
+    if constexpr (kOut == Q8_TYPE_MX4) {
+        static_assert(kOut != Q8_TYPE_MX4 || FN == 1 || FN == 2 || FN == 4, "wave tiles of a group, or of a half or a quarter of one");
+        constexpr int kPair = FN < 2 ? 1 : 2;  // blocks that one store takes
 #pragma unroll
         for (int i = 0; i < FM; ++i) {
             const int m = wm * TM + i * 32 + l32;
-            const int at = m < tile.rows ? m * row_bytes + 8 * hi : (int)kOutOfRange;
-            unsigned bytes = 0;
+            const unsigned row_at = m < tile.rows ? (unsigned)(m * row_bytes) : kOutOfRange;
+            const int nw = n0 + wn * TN;
+            if (nw >= N) break;  // columns come in whole groups of 128
+            unsigned bytes = 0;  // scale bytes, side by side in a group's word
 #pragma unroll
-            for (int j = 0; j < FN; ++j) {
-                const int nb = n0 + wn * TN + j * 32;
-                if (nb >= N) break;  // columns come in whole groups of 128
-                float v[16];
+            for (int j = 0; j < FN; j += kPair) {
+                unsigned c[kPair][2];
 #pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    const float4 b = bias ? *reinterpret_cast<const float4*>(bias + nb + 8 * q + 4 * hi) : float4{0, 0, 0, 0};
-                    v[4 * q] = __fadd_rn(acc[i][j][4 * q], b.x), v[4 * q + 1] = __fadd_rn(acc[i][j][4 * q + 1], b.y);
-                    v[4 * q + 2] = __fadd_rn(acc[i][j][4 * q + 2], b.z), v[4 * q + 3] = __fadd_rn(acc[i][j][4 * q + 3], b.w);
+                for (int h = 0; h < kPair; ++h) {
+                    float v[16];
+                    block_values(i, j + h, v);
+                    float a = __builtin_fabsf(v[0]);
+#pragma unroll
+                    for (int e = 1; e < 15; e += 2) a = __builtin_elementwise_maximum(__builtin_elementwise_maximum(a, __builtin_fabsf(v[e])), __builtin_fabsf(v[e + 1]));
+                    a = __builtin_elementwise_maximum(a, __builtin_fabsf(v[15]));
+                    const v2u both = __builtin_amdgcn_permlane32_swap(__float_as_uint(a), __float_as_uint(a), false, false);  // the two lanes of the row
+                    const unsigned byte = mx4_scale_byte(max(both[0], both[1]));
+                    c[h][0] = mx4_codes8(v, byte), c[h][1] = mx4_codes8(v + 8, byte);
+                    bytes |= byte << (8 * (j + h));
                 }
-                if (gelu) {
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) v[e] = gelu_erf(v[e]);
+                // Columns 8q + 4hi .. +3 are 16 bits of word q of a block, this lane's the low or the high ones.  Lanes l and l + 32 exchange halves of two
+                // blocks, so that each holds four whole words of one.
+                if constexpr (kPair == 2) {
+                    const v2u p0 = __builtin_amdgcn_permlane32_swap(c[0][0], c[1][0], false, false), p1 = __builtin_amdgcn_permlane32_swap(c[0][1], c[1][1], false, false);
+                    const v4u w = {(p0[0] & 0xffffu) | (p0[1] << 16), (p0[0] >> 16) | (p0[1] & 0xffff0000u), (p1[0] & 0xffffu) | (p1[1] << 16), (p1[0] >> 16) | (p1[1] & 0xffff0000u)};
+                    __builtin_amdgcn_raw_buffer_store_b128(w, ry, row_at + (unsigned)((nw + (j + hi) * 32) / 2), 0, 0);
+                } else {
+                    const v2u p0 = __builtin_amdgcn_permlane32_swap(c[0][0], c[0][1], false, false);
+                    __builtin_amdgcn_raw_buffer_store_b64(v2u{(p0[0] & 0xffffu) | (p0[1] << 16), (p0[0] >> 16) | (p0[1] & 0xffff0000u)}, ry, row_at + (unsigned)((nw + j * 32) / 2 + 8 * hi), 0, 0);
                 }
-                unsigned amax = 0;
-#pragma unroll
-                for (int e = 0; e < 16; ++e) amax = max(amax, f32_abs_bits(v[e]));
-                amax = max(amax, (unsigned)__shfl_xor((int)amax, 32));
-                const unsigned byte = mx4_scale_byte(amax);
-                // columns 8q + 4hi .. +3 are 16 bits of word q, this lane's the low or the high ones; each lane stores two of the four words
-                const unsigned c0 = mx4_codes8(v, byte), c1 = mx4_codes8(v + 8, byte);
-                const unsigned got = (unsigned)__shfl_xor((int)(hi ? c0 : c1), 32);
-                const unsigned low = hi ? got : c0, high = hi ? c1 : got;
-                const unsigned w0 = (low & 0xffffu) | (high << 16), w1 = (low >> 16) | (high & 0xffff0000u);
-                typedef unsigned v2u __attribute__((ext_vector_type(2)));
-                __builtin_amdgcn_raw_buffer_store_b64(v2u{w0, w1}, ry, at < 0 ? at : at + nb / 2, 0, 0);
-                bytes |= byte << (8 * (j % 4));
-                constexpr int kRun = FN < 4 ? FN : 4;  // a wave's blocks of a group, whose scale bytes lie side by side
-                if ((j + 1) % kRun == 0) {
-                    if (hi == 0 && m < tile.rows) {
-                        uint8_t* s = p.y_scales + ((int64_t)(nb / kMxGroup) * p.M + tile.row + m) * 4 + (nb % kMxGroup) / 32 - (kRun - 1);
-                        if constexpr (kRun == 4)
-                            *reinterpret_cast<unsigned*>(s) = bytes;
-                        else if constexpr (kRun == 2)
-                            *reinterpret_cast<unsigned short*>(s) = (unsigned short)bytes;
-                        else
-                            *s = (uint8_t)bytes;
-                    }
-                    bytes = 0;
-                }
+            }
+            if (hi == 0 && m < tile.rows) {
+                uint8_t* s = p.y_scales + ((int64_t)(nw / kMxGroup) * p.M + tile.row + m) * 4 + (nw % kMxGroup) / 32;
+                if constexpr (FN == 4)
+                    *reinterpret_cast<unsigned*>(s) = bytes;
+                else if constexpr (FN == 2)
+                    *reinterpret_cast<unsigned short*>(s) = (unsigned short)bytes;
+                else
+                    *s = (uint8_t)bytes;
             }
         }
     } else {
-        static_assert(kSwap || FN == 1 || FN == 2 || FN == 4, "wave tiles of whole or half groups");
-        const float sx = Op::kMx4 ? 0.0f : p.sx[0], next_scale = kOut == Q8_TYPE_I8 ? p.next_scale[0] : 0.0f;
-        const __amdgpu_buffer_rsrc_t ry =
-            __builtin_amdgcn_make_buffer_rsrc(static_cast<char*>(p.y) + (int64_t)tile.row * N * kSize, 0, tile.rows * N * kSize, 0x00020000);
-        float famax = 0.0f;
+        // Through LDS to whole 128-byte lines, 4 KiB of the stage buffers a wave: 32 rows of 32 fp32 or 64 bf16 columns (int8: 32 columns, 32-byte
+        // rows).  16-byte chunk c of row m lies at chunk c ^ (m % 8), free of bank conflicts both ways.
+        // Stores straight from the accumulators, 32 bytes of 32 rows each, ask four times as much of the L2, which takes a request a cycle
+        // and channel: 12288 x 1024 -> 4096 + GELU to fp32 71 us, this way 63.
+        constexpr int kPer = kOut == Q8_TYPE_BF16 && FN % 2 == 0 ? 2 : 1;  // blocks of a pass
+        constexpr int kRowBytes = 32 * kPer * kSize, kChunks = kRowBytes / 16;
+        static_assert(kSlots * SLOT >= NW * 32 * kRowBytes, "a pass of every wave fits the stage buffers");
+        char* mine = lds + wave * 32 * kRowBytes;
+        // a row's chunks start on 16 bytes and none crosses its end
+        const bool wide = row_bytes % 16 == 0 && reinterpret_cast<uintptr_t>(p.y) % 16 == 0;
+        if (tail) __syncthreads();  // the waves are done with the stage
 #pragma unroll
-        for (int j = 0; j < FN; ++j) {
-            const int n = n0 + wn * TN + j * 32 + l32;
-            const bool inside = n < N;
-            const ProductColumn c = product_column<Op>(p, tile.group, min(n, N - 1), sx);
+        for (int i = 0; i < FM; ++i) {
 #pragma unroll
-            for (int i = 0; i < FM; ++i) {
-                const int m = wm * TM + i * 32 + 4 * hi;
-                float v[16];
+            for (int j = 0; j < FN; j += kPer) {
+                const int nb = n0 + wn * TN + j * 32;
 #pragma unroll
-                for (int e = 0; e < 16; ++e) v[e] = product_value<Op>(acc[i][j][e], c);
-                if (gelu) {
+                for (int h = 0; h < kPer; ++h) {
+                    float v[16];
+                    block_values(i, j + h, v);
+                    if (wide) {
+                        const auto put = [&](int chunk_at) { return mine + l32 * kRowBytes + ((chunk_at ^ (l32 % kChunks)) << 4); };
+                        if constexpr (kOut == Q8_TYPE_F32) {
 #pragma unroll
-                    for (int e = 0; e < 16; ++e) v[e] = gelu_erf(v[e]);
-                }
-                if constexpr (!Op::kMx4) {
-                    if (p.flags & Q8_EPI_ABSMAX) {
+                            for (int q = 0; q < 4; ++q) *reinterpret_cast<float4*>(put(2 * q + hi)) = float4{v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]};
+                        } else if constexpr (kOut == Q8_TYPE_BF16) {
+                            // lanes l and l + 32 hold columns 0-3 and 4-7 of one 8 and of the next, and exchange halves
 #pragma unroll
-                        for (int e = 0; e < 16; ++e)
-                            if (inside && m + 8 * (e >> 2) + (e & 3) < tile.rows) famax = __builtin_fmaxf(famax, __builtin_fabsf(v[e]));
+                            for (int q = 0; q < 4; q += 2) {
+                                const float* u = v + 4 * q;
+                                const v2u a = __builtin_amdgcn_permlane32_swap(f32_to_bf16x2(u[0], u[1]), f32_to_bf16x2(u[4], u[5]), false, false);
+                                const v2u b = __builtin_amdgcn_permlane32_swap(f32_to_bf16x2(u[2], u[3]), f32_to_bf16x2(u[6], u[7]), false, false);
+                                *reinterpret_cast<v4u*>(put(4 * h + q + hi)) = v4u{a[0], b[0], a[1], b[1]};
+                            }
+                        } else {
+#pragma unroll
+                            for (int q = 0; q < 4; ++q) {
+                                unsigned w = 0;
+#pragma unroll
+                                for (int e = 0; e < 4; ++e) w |= ((unsigned)quantize_code(v[4 * q + e], next_scale) & 0xffu) << (8 * e);
+                                *reinterpret_cast<unsigned*>(put(q / 2) + 8 * (q % 2) + 4 * hi) = w;
+                            }
+                        }
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) {
+                            const int m = wm * TM + i * 32 + l32, n = nb + h * 32 + 8 * (e >> 2) + 4 * hi + (e & 3);
+                            const unsigned to = m < tile.rows && n < N ? (unsigned)(m * row_bytes + n * kSize) : kOutOfRange;
+                            if constexpr (kOut == Q8_TYPE_F32)
+                                __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(v[e]), ry, to, 0, 0);
+                            else if constexpr (kOut == Q8_TYPE_BF16)
+                                __builtin_amdgcn_raw_buffer_store_b16(f32_to_bf16(v[e]), ry, to, 0, 0);
+                            else
+                                __builtin_amdgcn_raw_buffer_store_b8((unsigned char)quantize_code(v[e], next_scale), ry, to, 0, 0);
+                        }
                     }
                 }
+                if (wide) {
+                    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");  // the lanes read what other lanes of this wave wrote
+                    __builtin_amdgcn_wave_barrier();
 #pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                    const int r = m + 8 * (e >> 2) + (e & 3);
-                    const int at = inside ? (r * N + n) * kSize : (int)kOutOfRange;  // rows behind the tile's are out of the descriptor's range
-                    if constexpr (kOut == Q8_TYPE_F32)
-                        __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(v[e]), ry, at, 0, 0);
-                    else if constexpr (kOut == Q8_TYPE_BF16)
-                        __builtin_amdgcn_raw_buffer_store_b16(f32_to_bf16(v[e]), ry, at, 0, 0);
-                    else
-                        __builtin_amdgcn_raw_buffer_store_b8((unsigned char)quantize_code(v[e], next_scale), ry, at, 0, 0);
+                    for (int t = 0; t < 32 * kChunks / 64; ++t) {
+                        const int row = t * (64 / kChunks) + lane / kChunks, c = lane % kChunks, m = wm * TM + i * 32 + row, n = nb + c * (16 / kSize);
+                        const v4u w = *reinterpret_cast<const v4u*>(mine + row * kRowBytes + ((c ^ (row % kChunks)) << 4));
+                        __builtin_amdgcn_raw_buffer_store_b128(w, ry, m < tile.rows && n < N ? (unsigned)(m * row_bytes + n * kSize) : kOutOfRange, 0, 0);
+                    }
+                    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");  // and are done before the next pass writes
+                    __builtin_amdgcn_wave_barrier();
                 }
             }
         }
-        if constexpr (!Op::kMx4)
-            if (p.flags & Q8_EPI_ABSMAX) publish_amax<NW>(__float_as_uint(famax), reinterpret_cast<unsigned*>(lds), p.out_amax);
     }
+    if constexpr (!Op::kMx4)
+        if (p.flags & Q8_EPI_ABSMAX) publish_amax<NW>(__float_as_uint(famax), reinterpret_cast<unsigned*>(lds), p.out_amax);
 #endif
 }
 
-template <class Op, int BM, int BN, int WGM, int WGN, int kSlots, int kWgs>
+template <class Op, int BM, int BN, int WGM, int WGN, int kSlots, int kAhead, int kWgs>
 int launch_product_tile(const Product& p, hipStream_t st)
 {
     const int64_t tiles_n = (p.N + BN - 1) / BN, tiles = row_tiles(p.M, p.group_rows, p.n_groups, BM) * tiles_n;
@@ -312,7 +390,7 @@ int launch_product_tile(const Product& p, hipStream_t st)
     const dim3 grid((unsigned)tiles), block(WGM * WGN * 64);
     const unsigned group_m = 8;
 #define Q8_PT_LAUNCH(OUT) \
-    hipLaunchKernelGGL((product_tile_kernel<Op, BM, BN, WGM, WGN, kSlots, kWgs, OUT>), grid, block, 0, st, p, (unsigned)tiles_n, group_m)
+    hipLaunchKernelGGL((product_tile_kernel<Op, BM, BN, WGM, WGN, kSlots, kAhead, kWgs, OUT>), grid, block, 0, st, p, (unsigned)tiles_n, group_m)
     if (p.y_type == Q8_TYPE_F32) {
         Q8_PT_LAUNCH(Q8_TYPE_F32);
     } else if constexpr (Op::kMx4) {

@@ -64,11 +64,26 @@ __device__ __forceinline__ unsigned quad_max_u32(unsigned v)
 __device__ __forceinline__ float bf16_to_f32(unsigned short b) { return __uint_as_float((unsigned)b << 16); }
 
 // Round to nearest even; a NaN stays one.
-__device__ __forceinline__ unsigned short f32_to_bf16(float f)
+__device__ __forceinline__ unsigned f32_to_bf16x2(float low, float high)
 {
-    const unsigned u = __float_as_uint(f);
-    if ((u & 0x7fffffffu) > 0x7f800000u) return (unsigned short)((u >> 16) | 0x40u);
-    return (unsigned short)((u + 0x7fffu + ((u >> 16) & 1u)) >> 16);
+    typedef float v2f __attribute__((ext_vector_type(2)));
+    typedef __bf16 v2b __attribute__((ext_vector_type(2)));
+    return __builtin_bit_cast(unsigned, __builtin_convertvector((v2f{low, high}), v2b));
+}
+__device__ __forceinline__ unsigned short f32_to_bf16(float f) { return __builtin_bit_cast(unsigned short, (__bf16)f); }
+
+// gelu_erf (q8_device.h) with a NaN for a NaN: the same polynomial and roundings, but the two comparisons are the ones that pass a NaN on,
+// which also spares the compiler the operation that quiets their operands.
+__device__ __forceinline__ float gelu_erf_nan(float v)
+{
+    const float a = __builtin_elementwise_minimum(__builtin_fabsf(v), 6.0f);
+    float p = __builtin_fmaf(3.309277963e-05f, a, -7.692193612e-04f);
+    p = __builtin_fmaf(p, a, 8.080715314e-03f);
+    p = __builtin_fmaf(p, a, -5.341210216e-02f);
+    p = __builtin_fmaf(p, a, -4.587709606e-01f);
+    p = __builtin_fmaf(p, a, -1.151201725e+00f);
+    p = __builtin_fmaf(p, a, -9.999930859e-01f);
+    return __builtin_fmaf(-a, __builtin_amdgcn_exp2f(p), __builtin_elementwise_maximum(v, 0.0f));
 }
 
 }  // namespace q8

@@ -208,12 +208,19 @@ def test_linear_follows_nan_and_infinity(q8, variant, M):
     g = np.random.default_rng(9)
     x, w = tensor(g, M, 384, 0.3), tensor(g, 260, 384, 0.3)
     x[2, 40], x[4, 383], w[7, 0], w[259, 200] = np.nan, np.inf, -np.inf, np.nan
-    y = torch.empty((M, 260), device="cuda")
-    q8.q8_mx4_linear(*quantized(q8, dev(x)), *quantized(q8, dev(w)), None, y)
-    bad = np.isnan(host(y))
     want = np.zeros((M, 260), bool)
     want[[2, 4]], want[:, [7, 259]] = True, True
-    np.testing.assert_array_equal(bad, want)
+    for flags in (0, q8.EPI_GELU):
+        y = torch.empty((M, 260), device="cuda")
+        q8.q8_mx4_linear(*quantized(q8, dev(x)), *quantized(q8, dev(w)), None, y, flags=flags)
+        np.testing.assert_array_equal(np.isnan(host(y)), want)
+    # a bias that is infinite or NaN, and outputs in codes: the block of 32 columns is NaN
+    b = torch.zeros(256, device="cuda")
+    b[3], b[100] = float("inf"), float("nan")
+    xq, wq = quantized(q8, dev(tensor(g, M, 384, 0.3))), quantized(q8, dev(tensor(g, 256, 384, 0.3)))
+    codes, scales = q8.mx4_empty(M, 256)
+    q8.q8_mx4_linear(*xq, *wq, b, codes, y_scales=scales, flags=q8.EPI_GELU)
+    assert (scales[0, :, 0] == 255).all() and (scales[0, :, 3] == 255).all() and int((scales == 255).sum()) == 2 * M
 
 
 # ---- grouped products ----------------------------------------------------------------------------------------------------
