@@ -416,7 +416,8 @@ q8_status q8_mx4_linear(const uint8_t* xq, const uint8_t* xs, const uint8_t* wq,
                         int64_t N, int64_t K, void* y, int y_type, uint8_t* y_scales, uint32_t flags, void* stream);
 
 /*
- * The same on an fp32 or bf16 x [M,K], quantized on the way: the results of q8_mx4_quantize followed by q8_mx4_linear.
+ * The same on an fp32 or bf16 x [M,K], quantized on the way: the results of q8_mx4_quantize followed by q8_mx4_linear, but for the order in which
+ * the fp32 sums are taken.  Two launches, or one for a handful of rows (M <= 32, K <= 4096, M * K <= 32768).
  *   xq_work uint8[M * Q8_MX4_CODE_BYTES(K)] (16-byte aligned), xs_work uint8[M * Q8_MX4_SCALE_BYTES(K)] (4-byte aligned): scratch, contents
  *   unspecified on return.
  */

@@ -492,6 +492,12 @@ q8_status q8_mx4_linear_dynamic(const void* x, int x_type, const uint8_t* wq, co
             if (overlap(r.p, r.bytes, xq_work, c_bytes) || overlap(r.p, r.bytes, xs_work, s_bytes)) return Q8_ERR_OVERLAP;
         const int64_t x_bytes = M * K * type_bytes(x_type), y_bytes = y_type == Q8_TYPE_MX4 ? M * Q8_MX4_CODE_BYTES(N) : M * N * type_bytes(y_type);
         if (overlap(x, x_bytes, y, y_bytes) || (y_type == Q8_TYPE_MX4 && overlap(x, x_bytes, y_scales, M * Q8_MX4_SCALE_BYTES(N)))) return Q8_ERR_OVERLAP;
+        if (q8::mx4_few_eligible(M, N, K)) {
+            if (!x) return Q8_ERR_NULL;
+            if (misaligned(x, (unsigned)type_bytes(x_type))) return Q8_ERR_ALIGN;
+            if (overlap(x, x_bytes, xq_work, c_bytes) || overlap(x, x_bytes, xs_work, s_bytes) || overlap(xq_work, c_bytes, xs_work, s_bytes)) return Q8_ERR_OVERLAP;
+            return q8::launch_mx4_few(x, x_type == Q8_TYPE_BF16, K, p, as_stream(stream)) ? Q8_ERR_LAUNCH : Q8_OK;
+        }
         s = q8_mx4_quantize(x, x_type, M, K, xq_work, xs_work, stream);
         if (s != Q8_OK) return s;
     }

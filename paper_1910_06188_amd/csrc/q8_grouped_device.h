@@ -163,4 +163,41 @@ __device__ __forceinline__ unsigned half_wave_max_u32(unsigned v)
     return max(v, (unsigned)__shfl_xor((int)v, 16));
 }
 
+// The epilogue of a 32x32 tile whose KW partial sums, one of each wave, lie in LDS at part[(w * 32 + row) * pitch + column].  They are added in the order
+// of the waves.  A thread keeps its column, and a row's 32 lanes stay together.  Returns the bits of the largest |y| of this thread.
+template <class Op, int KW>
+__device__ __forceinline__ unsigned finish_tile(const Product& p, const RowTile& tile, int64_t n0, const typename Op::Sum* part, int pitch)
+{
+    const int l32 = threadIdx.x & 31;
+    const int64_t n = n0 + l32;
+    const bool gelu = p.flags & Q8_EPI_GELU, requant = p.flags & Q8_EPI_REQUANT;
+    unsigned amax = 0;
+    if (n >= p.N) return amax;
+    const float sx = Op::kMx4 ? 0.0f : p.sx[0], next_scale = requant ? p.next_scale[0] : 0.0f;
+    const ProductColumn c = product_column<Op>(p, tile.group, n, sx);
+    for (int r = threadIdx.x / 32; r < tile.rows; r += KW * 2) {
+        typename Op::Sum sum = part[r * pitch + l32];
+#pragma unroll
+        for (int w = 1; w < KW; ++w) sum += part[(w * 32 + r) * pitch + l32];
+        float y = product_value<Op>(sum, c);
+        if (gelu) y = product_gelu<Op>(y);
+        const int64_t m = tile.row + r, at = m * p.N + n;
+        if (p.y_type == Q8_TYPE_MX4) {
+            const unsigned byte = mx4_scale_byte(half_wave_max_u32(f32_abs_bits(y)));
+            const float next = __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(y), 0xB1, 0xf, 0xf, true));
+            const unsigned code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(0, y, next, mx4_scale(byte), 0);
+            if (l32 % 2 == 0) static_cast<uint8_t*>(p.y)[at / 2] = byte == kMxNan ? 0 : (uint8_t)code;
+            if (l32 == 0) p.y_scales[((n / kMxGroup) * p.M + m) * 4 + (n % kMxGroup) / 32] = (uint8_t)byte;
+        } else if (p.y_type == Q8_TYPE_BF16) {
+            static_cast<unsigned short*>(p.y)[at] = f32_to_bf16(y);
+        } else if (requant) {
+            static_cast<int8_t*>(p.y)[at] = (int8_t)quantize_code(y, next_scale);
+        } else {
+            static_cast<float*>(p.y)[at] = y;
+        }
+        amax = max(amax, f32_abs_bits(y));
+    }
+    return amax;
+}
+
 }  // namespace q8

@@ -125,36 +125,7 @@ __global__ __launch_bounds__(KW * 64, 4) void product_direct_kernel(Product p, u
     for (int e = 0; e < 16; ++e) part[(wave * kPdTile + 8 * (e >> 2) + 4 * hi + (e & 3)) * kRow + l32] = acc[e];
     __syncthreads();
 
-    constexpr int kRowStep = KW * 64 / kPdTile;
-    const int64_t n = n0 + l32;
-    const bool gelu = p.flags & Q8_EPI_GELU, requant = p.flags & Q8_EPI_REQUANT;
-    unsigned amax = 0;
-    if (n < p.N) {
-        const float sx = Op::kMx4 ? 0.0f : p.sx[0], next_scale = requant ? p.next_scale[0] : 0.0f;
-        const ProductColumn c = product_column<Op>(p, tile.group, n, sx);
-        for (int r = threadIdx.x / kPdTile; r < tile.rows; r += kRowStep) {  // a row's 32 lanes stay together
-            Sum sum = part[r * kRow + l32];
-#pragma unroll
-            for (int w = 1; w < KW; ++w) sum += part[(w * kPdTile + r) * kRow + l32];
-            float y = product_value<Op>(sum, c);
-            if (gelu) y = product_gelu<Op>(y);
-            const int64_t m = tile.row + r, at = m * p.N + n;
-            if (p.y_type == Q8_TYPE_MX4) {
-                const unsigned byte = mx4_scale_byte(half_wave_max_u32(f32_abs_bits(y)));
-                const float next = __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(y), 0xB1, 0xf, 0xf, true));
-                const unsigned code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(0, y, next, mx4_scale(byte), 0);
-                if (l32 % 2 == 0) static_cast<uint8_t*>(p.y)[at / 2] = byte == kMxNan ? 0 : (uint8_t)code;
-                if (l32 == 0) p.y_scales[((n / kMxGroup) * p.M + m) * 4 + (n % kMxGroup) / 32] = (uint8_t)byte;
-            } else if (p.y_type == Q8_TYPE_BF16) {
-                static_cast<unsigned short*>(p.y)[at] = f32_to_bf16(y);
-            } else if (requant) {
-                static_cast<int8_t*>(p.y)[at] = (int8_t)quantize_code(y, next_scale);
-            } else {
-                static_cast<float*>(p.y)[at] = y;
-            }
-            amax = max(amax, f32_abs_bits(y));
-        }
-    }
+    unsigned amax = finish_tile<Op, KW>(p, tile, n0, part, kRow);
     if (p.flags & Q8_EPI_ABSMAX) {
         amax = wave_max_u32(amax);
         if (lane == 0) wave_amax[wave] = amax;

@@ -96,6 +96,10 @@ int launch_product(bool mx4, const Product& p, hipStream_t st);
 // 32x32 tiles for any size and alignment (q8_grouped_direct.hip).
 int launch_product_direct(bool mx4, const Product& p, hipStream_t st);
 
+// A 4-bit layer of few rows of fp32 or bf16, quantized in the same launch (q8_mx4_few.hip); p.x and p.xs are not looked at.
+bool mx4_few_eligible(int64_t M, int64_t N, int64_t K);
+int launch_mx4_few(const void* x, bool bf16, int64_t K, const Product& p, hipStream_t st);
+
 // The router of a mixture of experts and the sum behind it (q8_route.hip).
 int launch_route(const float* logits, int64_t T, int n_experts, int k, int32_t* experts, float* gates, int32_t* group_rows, int32_t* rows,
                  int32_t* slots, int32_t* work, hipStream_t st);

@@ -10,57 +10,27 @@
 
 namespace q8 {
 
-typedef float v4f __attribute__((ext_vector_type(4)));
 typedef unsigned v4u __attribute__((ext_vector_type(4)));
 typedef unsigned short u16;
 
-// Elements k .. k+7 of a row, zeros from K on.  kVec: k + 7 < K and the address is a multiple of 16 bytes.
-template <bool kVec>
-__device__ __forceinline__ void load8(const float* p, int left, float* v)
-{
-    if constexpr (kVec) {
-        const v4f a = *reinterpret_cast<const v4f*>(p), b = *reinterpret_cast<const v4f*>(p + 4);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = a[i], v[4 + i] = b[i];
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = i < left ? p[i] : 0.0f;
-    }
-}
-template <bool kVec>
-__device__ __forceinline__ void load8(const u16* p, int left, float* v)
-{
-    if constexpr (kVec) {
-        const v4u a = *reinterpret_cast<const v4u*>(p);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) v[2 * i] = __uint_as_float(a[i] << 16), v[2 * i + 1] = __uint_as_float(a[i] & 0xffff0000u);
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = i < left ? bf16_to_f32(p[i]) : 0.0f;
-    }
-}
-
 // The values of E2M1 codes have two significant bits: rounding them to bf16 changes nothing (2^-128, the smallest, is a bf16 number).
-template <bool kVec>
 __device__ __forceinline__ void store8(float* p, int left, const float* v)
 {
-    if constexpr (kVec) {
-        *reinterpret_cast<v4f*>(p) = v4f{v[0], v[1], v[2], v[3]};
-        *reinterpret_cast<v4f*>(p + 4) = v4f{v[4], v[5], v[6], v[7]};
+    if (left >= 8) {
+        __builtin_memcpy(p, v, 32);
     } else {
 #pragma unroll
         for (int i = 0; i < 8; ++i)
             if (i < left) p[i] = v[i];
     }
 }
-template <bool kVec>
 __device__ __forceinline__ void store8(u16* p, int left, const float* v)
 {
-    if constexpr (kVec) {
-        v4u a;
+    if (left >= 8) {
+        unsigned a[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) a[i] = (__float_as_uint(v[2 * i]) >> 16) | (__float_as_uint(v[2 * i + 1]) & 0xffff0000u);
-        *reinterpret_cast<v4u*>(p) = a;
+        __builtin_memcpy(p, a, 16);
     } else {
 #pragma unroll
         for (int i = 0; i < 8; ++i)
@@ -68,55 +38,95 @@ __device__ __forceinline__ void store8(u16* p, int left, const float* v)
     }
 }
 
-__device__ __forceinline__ unsigned amax8(const float* v)
+// The general kernel.  kCodes: codes and scales; else the values, in place if x is xq.  A wave takes kUnits times four neighbouring rows of one
+// group, all loads in front; the rows of a workgroup fill half a 128-byte line of scales or all of it.
+template <class T, bool kCodes, int kWaves, int kUnits>
+__global__ __launch_bounds__(kWaves * 64) void mx4_quantize_kernel(const T* x, int64_t M, int64_t K, unsigned groups, uint8_t* __restrict__ codes,
+                                                                   uint8_t* __restrict__ scales, T* xq)
 {
-    unsigned m = 0;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) m = max(m, __float_as_uint(v[i]) & 0x7fffffffu);
-    return m;
-}
-
-constexpr int kMxThreads = 256;
-constexpr int kMxRows = kMxThreads / 16;  // rows of a workgroup's step, one group of each
-
-// kCodes: codes and scales; else the values, in place if x is xq.
-template <class T, bool kVec, bool kCodes>
-__global__ __launch_bounds__(kMxThreads) void mx4_quantize_kernel(const T* x, int64_t M, int64_t K, unsigned groups, uint8_t* __restrict__ codes,
-                                                                  uint8_t* __restrict__ scales, T* xq)
-{
+    constexpr int kRows = kWaves * 4;  // from one unit to the next
     const unsigned group = blockIdx.x % groups;
-    const int64_t row = (int64_t)(blockIdx.x / groups) * kMxRows + threadIdx.x / 16;
-    if (row >= M) return;  // whole quads leave
+    const int64_t row0 = (int64_t)(blockIdx.x / groups) * (kRows * kUnits) + threadIdx.x / 16;
     const int in_group = (threadIdx.x % 16) * 8;
     const int64_t k = (int64_t)group * kMxGroup + in_group;
     const int left = (int)min(K - k, (int64_t)8);
-    float v[8];
-    if (kVec ? left > 0 : true)
-        load8<kVec>(x + row * K + k, left, v);
-    else
-        for (int i = 0; i < 8; ++i) v[i] = 0.0f;
-    const unsigned byte = mx4_scale_byte(quad_max_u32(amax8(v)));
-    const unsigned c = mx4_codes8(v, byte);
-    if constexpr (kCodes) {
-        *reinterpret_cast<unsigned*>(codes + (row * groups + group) * (kMxGroup / 2) + in_group / 2) = c;
-        if (threadIdx.x % 4 == 0) scales[((int64_t)group * M + row) * 4 + in_group / 32] = (uint8_t)byte;
-    } else if (left > 0) {
-        mx4_values8(c, byte, v);
-        store8<kVec>(xq + row * K + k, left, v);
+    float v[kUnits][8];
+#pragma unroll
+    for (int u = 0; u < kUnits; ++u) {
+        const int64_t row = row0 + u * kRows;
+        if (row < M && left > 0) {
+            load8(x + row * K + k, left, v[u]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[u][i] = 0.0f;
+        }
     }
+#pragma unroll
+    for (int u = 0; u < kUnits; ++u) {
+        const int64_t row = row0 + u * kRows;
+        const unsigned byte = mx4_scale_byte(quad_max_u32(amax8(v[u])));
+        const unsigned c = mx4_codes8(v[u], byte);
+        if (row >= M) return;
+        if constexpr (kCodes) {
+            *reinterpret_cast<unsigned*>(codes + (row * groups + group) * (kMxGroup / 2) + in_group / 2) = c;
+            if (threadIdx.x % 4 == 0) scales[((int64_t)group * M + row) * 4 + in_group / 32] = (uint8_t)byte;
+        } else if (left > 0) {
+            mx4_values8(c, byte, v[u]);
+            store8(xq + row * K + k, left, v[u]);
+        }
+    }
+}
+
+// Values of rows that are whole blocks: the tensor is one run of blocks, and a lane takes the 16 bytes of its own place in it, workgroups of
+// one wave in address order, which moves the most bytes on this part (12288 x 4096 to bf16 31 us, to fp32 60, the time of a copy; the general kernel 37 and 72).
+template <class T>
+__global__ __launch_bounds__(64) void mx4_fake_quantize_kernel(const T* x, T* xq, int64_t vectors)
+{
+    constexpr int kElems = 16 / sizeof(T);
+    const int64_t i = (int64_t)blockIdx.x * 64 + threadIdx.x;
+    if (i >= vectors) return;  // whole blocks leave
+    const v4u in = __builtin_nontemporal_load(reinterpret_cast<const v4u*>(x) + i);
+    float v[8];
+    if constexpr (kElems == 4) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = __uint_as_float(in[e]), v[4 + e] = 0.0f;
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[2 * e] = __uint_as_float(in[e] << 16), v[2 * e + 1] = __uint_as_float(in[e] & 0xffff0000u);
+    }
+    unsigned a = quad_max_u32(amax8(v));
+    if constexpr (kElems == 4) a = max(a, (unsigned)__builtin_amdgcn_update_dpp(0, (int)a, 0x141, 0xf, 0xf, true));  // row_half_mirror: the block's other quad
+    const unsigned byte = mx4_scale_byte(a);
+    mx4_values8(mx4_codes8(v, byte), byte, v);
+    v4u out;
+    if constexpr (kElems == 4) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) out[e] = __float_as_uint(v[e]);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) out[e] = (__float_as_uint(v[2 * e]) >> 16) | (__float_as_uint(v[2 * e + 1]) & 0xffff0000u);
+    }
+    __builtin_nontemporal_store(out, reinterpret_cast<v4u*>(xq) + i);
 }
 
 template <class T, bool kCodes>
 static int launch(const T* x, int64_t M, int64_t K, uint8_t* codes, uint8_t* scales, T* xq, hipStream_t st)
 {
-    const int64_t groups = mx4_groups(K), blocks = (M + kMxRows - 1) / kMxRows * groups;
-    if (blocks > 0x7fffffffLL) return 1;
-    // eight elements at a time where all of them start on 16 bytes
-    const bool vec = K % 8 == 0 && reinterpret_cast<uintptr_t>(x) % 16 == 0 && reinterpret_cast<uintptr_t>(xq) % 16 == 0;
-    if (vec)
-        hipLaunchKernelGGL((mx4_quantize_kernel<T, true, kCodes>), dim3((unsigned)blocks), dim3(kMxThreads), 0, st, x, M, K, (unsigned)groups, codes, scales, xq);
-    else
-        hipLaunchKernelGGL((mx4_quantize_kernel<T, false, kCodes>), dim3((unsigned)blocks), dim3(kMxThreads), 0, st, x, M, K, (unsigned)groups, codes, scales, xq);
+    constexpr int64_t kElems = 16 / sizeof(T);
+    const bool aligned = reinterpret_cast<uintptr_t>(x) % 16 == 0 && reinterpret_cast<uintptr_t>(xq) % 16 == 0;
+    if constexpr (!kCodes) {
+        const int64_t vectors = M * K / kElems;
+        if (aligned && K % 32 == 0 && vectors < (int64_t)1 << 32) {
+            hipLaunchKernelGGL(mx4_fake_quantize_kernel<T>, dim3((unsigned)((vectors + 63) / 64)), dim3(64), 0, st, x, xq, vectors);
+            return hipGetLastError() == hipSuccess ? 0 : 1;
+        }
+    }
+    const int64_t groups = mx4_groups(K);
+    // one unit for fp32 (12288 x 4096: 39.3 us, two 40.5, four 42.5), two for bf16, whose loads are half as wide (22.3, 20.5, 21.8)
+    constexpr int kWaves = 4, kUnits = sizeof(T) == 4 ? 1 : 2;
+    const int64_t blocks = (M + kWaves * 4 * kUnits - 1) / (kWaves * 4 * kUnits) * groups;
+    if (blocks * kWaves * 64 >= (int64_t)1 << 32) return 1;  // a launch is limited to 2^32 threads
+    hipLaunchKernelGGL((mx4_quantize_kernel<T, kCodes, kWaves, kUnits>), dim3((unsigned)blocks), dim3(kWaves * 64), 0, st, x, M, K, (unsigned)groups, codes, scales, xq);
     return hipGetLastError() == hipSuccess ? 0 : 1;
 }
 

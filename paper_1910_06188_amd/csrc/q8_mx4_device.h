@@ -86,4 +86,36 @@ __device__ __forceinline__ float gelu_erf_nan(float v)
     return __builtin_fmaf(-a, __builtin_amdgcn_exp2f(p), __builtin_elementwise_maximum(v, 0.0f));
 }
 
+// The first `left` (at most eight) of eight elements at whatever address, zeros behind them.
+__device__ __forceinline__ void load8(const float* p, int left, float* v)
+{
+    if (left >= 8) {
+        __builtin_memcpy(v, p, 32);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = i < left ? p[i] : 0.0f;
+    }
+}
+__device__ __forceinline__ void load8(const unsigned short* p, int left, float* v)
+{
+    if (left >= 8) {
+        unsigned a[4];
+        __builtin_memcpy(a, p, 16);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[2 * i] = __uint_as_float(a[i] << 16), v[2 * i + 1] = __uint_as_float(a[i] & 0xffff0000u);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = i < left ? bf16_to_f32(p[i]) : 0.0f;
+    }
+}
+
+// The largest |v|, as bits.
+__device__ __forceinline__ unsigned amax8(const float* v)
+{
+    unsigned m = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) m = max(m, __float_as_uint(v[i]) & 0x7fffffffu);
+    return m;
+}
+
 }  // namespace q8
