@@ -372,16 +372,6 @@ def q8_attention(qkv, B, S, heads, d, ctx=None, mask=None, scale=None, amax_slot
 
 # ---- 4-bit microscaled FC layers, FC layers grouped by expert, routing --------------------------------------------------
 
-_FLOAT_TYPES = {torch.float32: TYPE_F32, torch.bfloat16: TYPE_BF16}
-
-
-def _float_type(t, where: str) -> int:
-    code = _FLOAT_TYPES.get(t.dtype)
-    if code is None:
-        raise TypeError(f"{where}: takes float32 or bfloat16, not {t.dtype}")
-    return code
-
-
 def mx4_empty(*shape, device="cuda"):
     """Uninitialised codes and scales of a 4-bit tensor [rows, K], or of n of them [n, rows, K]."""
     *lead, rows, K = shape
@@ -390,110 +380,48 @@ def mx4_empty(*shape, device="cuda"):
             torch.empty((*lead, groups, rows, 4), dtype=torch.uint8, device=device))
 
 
-def _mx4_bad(codes, scales) -> bool:
-    """Whether codes [..., rows, 64 G] and scales [..., G, rows, 4] do not fit each other."""
-    return (codes.dim() < 2 or codes.shape[-1] % 64 != 0 or
-            tuple(scales.shape) != (*codes.shape[:-2], codes.shape[-1] // 64, codes.shape[-2], 4))
-
-
-def _product_output(y, y_scales, M, N, where: str) -> int:
-    """The type code of a 4-bit product's output: codes if there are scales for them, else fp32 or bf16."""
-    if y_scales is None:
-        if tuple(y.shape) != (M, N):
-            raise ValueError(f"{where}: y is [{M}, {N}]")
-        return _float_type(y, where)
-    if y.dtype != torch.uint8:
-        raise TypeError(f"{where}: codes are uint8")
-    if N % 128 != 0 or tuple(y.shape) != (M, N // 2) or _mx4_bad(y, y_scales):
-        raise ValueError(f"{where}: 4-bit outputs are codes [{M}, {N} / 2] and scales [{N} / 128, {M}, 4] of a width that is a multiple of 128")
-    return TYPE_MX4
-
+# Shapes, element types and devices are checked by the native module, which raises ValueError and TypeError.
 
 def q8_mx4_quantize(x, codes, scales, stream=None) -> None:
     """codes, scales = the 4-bit microscaled form of x [M, K] (fp32 or bf16); see mx4_empty."""
-    M, K = x.shape
-    if codes.shape[-1] != (K + 127) // 128 * 64 or codes.dim() != 2 or codes.shape[0] != M or _mx4_bad(codes, scales):
-        raise ValueError("q8_mx4_quantize: codes and scales do not fit x")
-    _ck(_binding.q8_mx4_quantize(x, _float_type(x, "q8_mx4_quantize"), M, K, codes, scales, _stream(stream)), "q8_mx4_quantize")
+    _ck(_binding.q8_mx4_quantize(x, codes, scales, _stream(stream)), "q8_mx4_quantize")
 
 
 def q8_mx4_fake_quantize(x, xq, stream=None) -> None:
     """xq = the values that the 4-bit codes of x [M, K] stand for, in x's type; xq may be x.  Its gradient is q8_ste_backward."""
-    M, K = x.shape
-    if xq.shape != x.shape or xq.dtype != x.dtype:
-        raise ValueError("q8_mx4_fake_quantize: xq and x differ in shape or type")
-    _ck(_binding.q8_mx4_fake_quantize(x, _float_type(x, "q8_mx4_fake_quantize"), M, K, xq, _stream(stream)), "q8_mx4_fake_quantize")
+    _ck(_binding.q8_mx4_fake_quantize(x, xq, _stream(stream)), "q8_mx4_fake_quantize")
 
 
 def q8_mx4_linear(xq, xs, wq, ws, bias, y, y_scales=None, flags=0, stream=None) -> None:
     """y = act(x w^T + bias) on 4-bit codes and scales of x and w; y fp32, bf16, or (with y_scales) 4-bit codes itself."""
-    if xq.dim() != 2 or wq.dim() != 2 or _mx4_bad(xq, xs) or _mx4_bad(wq, ws) or xq.shape[1] != wq.shape[1]:
-        raise ValueError("q8_mx4_linear: shape mismatch")
-    M, N, K = xq.shape[0], wq.shape[0], 2 * xq.shape[1]
-    if bias is not None and bias.numel() != N:
-        raise ValueError("q8_mx4_linear: bias size mismatch")
-    y_type = _product_output(y, y_scales, M, N, "q8_mx4_linear")
-    _ck(_binding.q8_mx4_linear(xq, xs, wq, ws, bias, M, N, K, y, y_type, y_scales, flags, _stream(stream)), "q8_mx4_linear")
+    _ck(_binding.q8_mx4_linear(xq, xs, wq, ws, bias, y, y_scales, flags, _stream(stream)), "q8_mx4_linear")
 
 
 def q8_mx4_linear_dynamic(x, wq, ws, bias, xq_work, xs_work, y, y_scales=None, flags=0, stream=None) -> None:
     """q8_mx4_linear of an fp32 or bf16 x [M, K], quantized on the way (xq_work, xs_work: scratch as mx4_empty(M, K) makes it)."""
-    M, K = x.shape
-    if wq.dim() != 2 or _mx4_bad(wq, ws) or wq.shape[1] != (K + 127) // 128 * 64:
-        raise ValueError("q8_mx4_linear_dynamic: shape mismatch")
-    if xq_work.numel() < M * wq.shape[1] or xs_work.numel() < M * wq.shape[1] // 16 or xq_work.dtype != torch.uint8 or xs_work.dtype != torch.uint8:
-        raise ValueError("q8_mx4_linear_dynamic: scratch of mx4_empty(M, K) needed")
-    N = wq.shape[0]
-    if bias is not None and bias.numel() != N:
-        raise ValueError("q8_mx4_linear_dynamic: bias size mismatch")
-    y_type = _product_output(y, y_scales, M, N, "q8_mx4_linear_dynamic")
-    _ck(_binding.q8_mx4_linear_dynamic(x, _float_type(x, "q8_mx4_linear_dynamic"), wq, ws, bias, M, N, K, xq_work, xs_work, y, y_type, y_scales, flags,
-                                       _stream(stream)), "q8_mx4_linear_dynamic")
+    _ck(_binding.q8_mx4_linear_dynamic(x, wq, ws, bias, xq_work, xs_work, y, y_scales, flags, _stream(stream)), "q8_mx4_linear_dynamic")
 
 
 def q8_mx4_linear_grouped(xq, xs, wq, ws, bias, group_rows, y, x_rows=None, y_scales=None, flags=0, stream=None) -> None:
     """FC layers of a mixture of experts on 4-bit codes: the rows of y belong to experts in order, group_rows[e] to expert e, and
     y[r] = act(x[x_rows[r]] w[e]^T + bias[e]).  Rows behind the last group's stay as they are."""
-    if xq.dim() != 2 or wq.dim() != 3 or _mx4_bad(xq, xs) or _mx4_bad(wq, ws) or xq.shape[1] != wq.shape[2]:
-        raise ValueError("q8_mx4_linear_grouped: shape mismatch")
-    E, N, K, M = wq.shape[0], wq.shape[1], 2 * xq.shape[1], y.shape[0]
-    if group_rows.numel() != E or (bias is not None and bias.numel() != E * N) or (xq.shape[0] if x_rows is None else x_rows.numel()) != M:
-        raise ValueError("q8_mx4_linear_grouped: group_rows, bias or x_rows size mismatch")
-    y_type = _product_output(y, y_scales, M, N, "q8_mx4_linear_grouped")
-    _ck(_binding.q8_mx4_linear_grouped(xq, xs, xq.shape[0], x_rows, wq, ws, bias, group_rows, E, M, N, K, y, y_type, y_scales, flags, _stream(stream)),
-        "q8_mx4_linear_grouped")
+    _ck(_binding.q8_mx4_linear_grouped(xq, xs, wq, ws, bias, group_rows, y, x_rows, y_scales, flags, _stream(stream)), "q8_mx4_linear_grouped")
 
 
 def q8_linear_grouped(xq, wq, bias, sx, sw, group_rows, y, x_rows=None, out_amax=None, next_scale=None, flags=0, stream=None) -> None:
     """FC layers of a mixture of experts on int8 codes: each expert's rows as q8_linear has them, with its own weights, scale and bias."""
-    if xq.dim() != 2 or wq.dim() != 3 or xq.shape[1] != wq.shape[2]:
-        raise ValueError("q8_linear_grouped: shape mismatch")
-    (E, N, K), M = wq.shape, y.shape[0]
-    if tuple(y.shape) != (M, N) or y.dtype != (torch.int8 if flags & EPI_REQUANT else torch.float32):
-        raise ValueError("q8_linear_grouped: y is [rows, N], fp32, or int8 with EPI_REQUANT")
-    if group_rows.numel() != E or sw.numel() != E or (bias is not None and bias.numel() != E * N) or (xq.shape[0] if x_rows is None else x_rows.numel()) != M:
-        raise ValueError("q8_linear_grouped: group_rows, scale, bias or x_rows size mismatch")
-    _ck(_binding.q8_linear_grouped(xq, xq.shape[0], x_rows, wq, bias, sx, sw, group_rows, E, M, N, K, y, out_amax, next_scale, flags,
-                                   _stream(stream)), "q8_linear_grouped")
+    _ck(_binding.q8_linear_grouped(xq, wq, bias, sx, sw, group_rows, y, x_rows, out_amax, next_scale, flags, _stream(stream)), "q8_linear_grouped")
 
 
 def q8_route(logits, experts, gates, group_rows, rows, slots, work, stream=None) -> None:
     """The k = experts.shape[1] experts of each token by logit, their softmax, and the (token, choice) pairs sorted by expert:
     group_rows and rows for the grouped products, slots for q8_combine."""
-    (T, E), k = logits.shape, experts.shape[1]
-    if tuple(experts.shape) != (T, k) or gates.numel() != T * k or group_rows.numel() != E or rows.numel() != T * k or slots.numel() != T * k:
-        raise ValueError("q8_route: shape mismatch")
-    if work.numel() < ROUTE_BLOCKS * E:
-        raise ValueError("q8_route: work holds ROUTE_BLOCKS * n_experts integers")
-    _ck(_binding.q8_route(logits, T, E, k, experts, gates, group_rows, rows, slots, work, _stream(stream)), "q8_route")
+    _ck(_binding.q8_route(logits, experts, gates, group_rows, rows, slots, work, _stream(stream)), "q8_route")
 
 
 def q8_combine(y, slots, gates, out, stream=None) -> None:
     """out[t] = sum over j of gates[t, j] * y[slots[t, j]]."""
-    (T, k), (R, N) = slots.shape, y.shape
-    if gates.numel() != T * k or tuple(out.shape) != (T, N) or out.dtype != y.dtype:
-        raise ValueError("q8_combine: shape or type mismatch")
-    _ck(_binding.q8_combine(y, R, slots, gates, T, k, N, out, _float_type(y, "q8_combine"), _stream(stream)), "q8_combine")
+    _ck(_binding.q8_combine(y, slots, gates, out, _stream(stream)), "q8_combine")
 
 
 def raw():
