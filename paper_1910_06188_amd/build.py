@@ -16,7 +16,7 @@ SOURCES = ["q8_api.hip", "q8_elementwise.hip", "q8_gemm.hip", "q8_embedding.hip"
            "q8_gemm_tile_64x64_w4.hip", "q8_gemm_ring_64x64_s2.hip", "q8_gemm_ring_64x64_s3.hip",
            "q8_gemm_ring_128x64_s2.hip", "q8_gemm_ring_128x128_s1.hip", "q8_gemm_ring_192x128_s1.hip",
            "q8_mx4.hip", "q8_grouped.hip", "q8_grouped_direct.hip", "q8_route.hip", "q8_mx4_few.hip",
-           "q8_grouped_tile_64x64_s1.hip", "q8_grouped_tile_64x128_s1.hip", "q8_grouped_tile_128x128_s1b.hip", "q8_grouped_tile_128x128_s1w2.hip", "q8_grouped_tile_256x128_s1.hip", "q8_grouped_tile_256x128_w8.hip", "q8_grouped_tile_256x256_s2.hip", "q8_grouped_tile_256x256_w4.hip"]
+           "q8_grouped_tile_64x64.hip", "q8_grouped_tile_64x128.hip", "q8_grouped_tile_128x128.hip", "q8_grouped_tile_256x256.hip"]
 OBJ_DIR = os.path.join(HERE, "_build")
 
 # -ffp-contract=off: the product x*S of Eq. 1 must be rounded on its own before the

@@ -8,27 +8,19 @@
 
 namespace q8 {
 
-int launch_product_64x64_s1(bool, const Product&, hipStream_t);
-int launch_product_64x128_s1(bool, const Product&, hipStream_t);
-int launch_product_128x128_s1b(bool, const Product&, hipStream_t);
-int launch_product_128x128_s1w2(bool, const Product&, hipStream_t);
-int launch_product_256x128_s1(bool, const Product&, hipStream_t);
-int launch_product_256x128_w8(bool, const Product&, hipStream_t);
-int launch_product_256x256_s2(bool, const Product&, hipStream_t);
-int launch_product_256x256_w4(bool, const Product&, hipStream_t);
+int launch_product_64x64(bool, const Product&, hipStream_t);
+int launch_product_64x128(bool, const Product&, hipStream_t);
+int launch_product_128x128(bool, const Product&, hipStream_t);
+int launch_product_256x256(bool, const Product&, hipStream_t);
 
 static const struct {
     int (*launch)(bool, const Product&, hipStream_t);
     int rows;
 } kTiles[] = {
-    {launch_product_64x64_s1, 64},
-    {launch_product_64x128_s1, 64},
-    {launch_product_128x128_s1b, 128},
-    {launch_product_128x128_s1w2, 128},
-    {launch_product_256x128_s1, 256},
-    {launch_product_256x128_w8, 256},
-    {launch_product_256x256_s2, 256},
-    {launch_product_256x256_w4, 256}};
+    {launch_product_64x64, 64},
+    {launch_product_64x128, 64},
+    {launch_product_128x128, 128},
+    {launch_product_256x256, 256}};
 
 static int g_variant = 0;
 void set_product_variant(int v) { g_variant = v; }

@@ -21,15 +21,18 @@ __device__ __forceinline__ void lds_dma4(v4i rsrc, unsigned voff, unsigned lds_a
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds" : : "s"(lds_addr), "v"(voff), "s"(rsrc) : "memory");
 }
 
-// The MFMA takes w as its first operand and x as its second, so that a lane holds one row of y and 16 columns of a 32x32 block, four
-// times four neighbours, and a block of the 4-bit format -- 32 neighbours of a row -- is two lanes', its largest magnitude one exchange away.
+// kOut: the type of y.  It decides which operand the MFMA takes first, that is, what a lane holds of a 32x32 block.
+//   fp32, bf16    x first: one column and 16 rows.  32 lanes store 32 neighbours of a row at once, whole 128-byte lines of fp32.  (With a row and 16
+//                 columns a lane, stores take 16 bytes a lane but 32 bytes of 32 rows each, four times the requests to the L2: 12288 x 1024 -> 4096 to fp32
+//                 59 us against 48; through LDS to whole lines 56, because LDS is what the MFMAs wait for.)
+//   4-bit, int8   w first: one row and four times four neighbouring columns.  A block of the 4-bit format -- 32 neighbours of a row -- is two
+//                 lanes', its largest magnitude one exchange away.
 // The bias is what the sums start from.
-//
-// kOut: the type of y.
 template <class Op, int BM, int BN, int WGM, int WGN, int kSlots, int kAhead, int kWgs, int kOut>
-__global__ __launch_bounds__(WGM* WGN * 64, kWgs* WGM* WGN / 4) void product_tile_kernel(Product p, unsigned tiles_n, unsigned group_m)
+__global__ __launch_bounds__(WGM* WGN * 64, kWgs* WGM* WGN / 4) void product_tile_kernel(Product p, unsigned tiles_n, unsigned group_m, int stream_out)
 {
 #if defined(__HIP_DEVICE_COMPILE__)
+    constexpr bool kRowLane = kOut == Q8_TYPE_MX4 || kOut == Q8_TYPE_I8;
     constexpr int NW = WGM * WGN;
     constexpr int TM = BM / WGM, TN = BN / WGN, FM = TM / 32, FN = TN / 32;
     constexpr int A_BYTES = BM * kBK, B_BYTES = BN * kBK, OPERANDS = A_BYTES + B_BYTES;
@@ -155,19 +158,28 @@ __global__ __launch_bounds__(WGM* WGN * 64, kWgs* WGM* WGN / 4) void product_til
     __builtin_amdgcn_s_waitcnt(waitcnt_vm_lgkm0(0));
     __syncthreads();
 
-    // Accumulator register e of lane l is column 8 (e / 4) + 4 (l / 32) + e % 4 and row l % 32 of its block.
+    // Accumulator register e of lane l is column 8 (e / 4) + 4 (l / 32) + e % 4 and row l % 32 of its block if kRowLane, else the other way round.
     typedef Sum v4s __attribute__((ext_vector_type(4)));
     typename Op::Acc acc[FM][FN];
 #pragma unroll
-    for (int j = 0; j < FN; ++j)
+    for (int j = 0; j < FN; ++j) {
+        if constexpr (kRowLane) {
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            const v4s c = *reinterpret_cast<const v4s*>(first + wn * TN + j * 32 + 8 * q + 4 * hi);
+            for (int q = 0; q < 4; ++q) {
+                const v4s c = *reinterpret_cast<const v4s*>(first + wn * TN + j * 32 + 8 * q + 4 * hi);
+#pragma unroll
+                for (int i = 0; i < FM; ++i)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) acc[i][j][4 * q + e] = c[e];
+            }
+        } else {
+            const Sum c = first[wn * TN + j * 32 + l32];
 #pragma unroll
             for (int i = 0; i < FM; ++i)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) acc[i][j][4 * q + e] = c[e];
+                for (int e = 0; e < 16; ++e) acc[i][j][e] = c;
         }
+    }
 
     // The MFMAs of a stage.  The fragments come kAhead - 1 steps ahead of them; as soon as the last are under way, `loads` may ask for the next stage.
     auto multiply = [&](const char* stage, auto loads) {
@@ -199,7 +211,10 @@ __global__ __launch_bounds__(WGM* WGN * 64, kWgs* WGM* WGN / 4) void product_til
             for (int i = 0; i < FM; ++i)
 #pragma unroll
                 for (int j = 0; j < FN; ++j)
-                    acc[i][j] = Op::template mfma<ks>(fb[ks % kAhead][j], fa[ks % kAhead][i], acc[i][j], Op::kMx4 ? sb[j] : 0, Op::kMx4 ? sa[i] : 0);
+                    if constexpr (kRowLane)
+                        acc[i][j] = Op::template mfma<ks>(fb[ks % kAhead][j], fa[ks % kAhead][i], acc[i][j], Op::kMx4 ? sb[j] : 0, Op::kMx4 ? sa[i] : 0);
+                    else
+                        acc[i][j] = Op::template mfma<ks>(fa[ks % kAhead][i], fb[ks % kAhead][j], acc[i][j], Op::kMx4 ? sa[i] : 0, Op::kMx4 ? sb[j] : 0);
             __builtin_amdgcn_sched_barrier(0);  // fragments of later steps would only take registers
         });
     };
@@ -234,7 +249,7 @@ __global__ __launch_bounds__(WGM* WGN * 64, kWgs* WGM* WGN / 4) void product_til
     const float r = Op::kMx4 ? 1.0f : dequant_factor(sx, p.sw[tile.group]);
     const float next_scale = kOut == Q8_TYPE_I8 ? p.next_scale[0] : 0.0f;
     float famax = 0.0f;
-    // Block (i, j) as fp32 values: row l32, columns 8 (e / 4) + 4 hi + e % 4.
+    // Block (i, j) as fp32 values.
     auto block_values = [&](int i, int j, float* v) {
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
@@ -249,11 +264,11 @@ __global__ __launch_bounds__(WGM* WGN * 64, kWgs* WGM* WGN / 4) void product_til
         }
         if constexpr (!Op::kMx4) {
             if (p.flags & Q8_EPI_ABSMAX) {
-                float a = 0.0f;
 #pragma unroll
-                for (int e = 0; e < 16; ++e)
-                    if (n0 + wn * TN + j * 32 + 8 * (e >> 2) + 4 * hi + (e & 3) < N) a = __builtin_fmaxf(a, __builtin_fabsf(v[e]));
-                if (wm * TM + i * 32 + l32 < tile.rows) famax = __builtin_fmaxf(famax, a);
+                for (int e = 0; e < 16; ++e) {
+                    const int along = 8 * (e >> 2) + 4 * hi + (e & 3), m = wm * TM + i * 32 + (kRowLane ? l32 : along), n = n0 + wn * TN + j * 32 + (kRowLane ? along : l32);
+                    if (m < tile.rows && n < N) famax = __builtin_fmaxf(famax, __builtin_fabsf(v[e]));
+                }
             }
         }
     };
@@ -304,78 +319,80 @@ __global__ __launch_bounds__(WGM* WGN * 64, kWgs* WGM* WGN / 4) void product_til
                     *s = (uint8_t)bytes;
             }
         }
-    } else {
-        // Through LDS to whole 128-byte lines, 4 KiB of the stage buffers a wave: 32 rows of 32 fp32 or 64 bf16 columns (int8: 32 columns, 32-byte
-        // rows).  16-byte chunk c of row m lies at chunk c ^ (m % 8), free of bank conflicts both ways.
-        // Stores straight from the accumulators, 32 bytes of 32 rows each, ask four times as much of the L2, which takes a request a cycle
-        // and channel: 12288 x 1024 -> 4096 + GELU to fp32 71 us, this way 63.
-        constexpr int kPer = kOut == Q8_TYPE_BF16 && FN % 2 == 0 ? 2 : 1;  // blocks of a pass
-        constexpr int kRowBytes = 32 * kPer * kSize, kChunks = kRowBytes / 16;
-        static_assert(kSlots * SLOT >= NW * 32 * kRowBytes, "a pass of every wave fits the stage buffers");
-        char* mine = lds + wave * 32 * kRowBytes;
-        // a row's chunks start on 16 bytes and none crosses its end
-        const bool wide = row_bytes % 16 == 0 && reinterpret_cast<uintptr_t>(p.y) % 16 == 0;
-        if (tail) __syncthreads();  // the waves are done with the stage
+    } else if constexpr (kOut == Q8_TYPE_I8) {
+        const bool wide = N % 4 == 0 && reinterpret_cast<uintptr_t>(p.y) % 4 == 0;  // four codes start on a word and no row ends inside them
 #pragma unroll
         for (int i = 0; i < FM; ++i) {
+            const int m = wm * TM + i * 32 + l32;
+            const unsigned row_at = m < tile.rows ? (unsigned)(m * row_bytes) : kOutOfRange;
 #pragma unroll
-            for (int j = 0; j < FN; j += kPer) {
-                const int nb = n0 + wn * TN + j * 32;
+            for (int j = 0; j < FN; ++j) {
+                float v[16];
+                block_values(i, j, v);
 #pragma unroll
-                for (int h = 0; h < kPer; ++h) {
-                    float v[16];
-                    block_values(i, j + h, v);
+                for (int q = 0; q < 4; ++q) {
+                    const int n = n0 + wn * TN + j * 32 + 8 * q + 4 * hi;
+                    unsigned code[4];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) code[e] = (unsigned)quantize_code(v[4 * q + e], next_scale) & 0xffu;
                     if (wide) {
-                        const auto put = [&](int chunk_at) { return mine + l32 * kRowBytes + ((chunk_at ^ (l32 % kChunks)) << 4); };
-                        if constexpr (kOut == Q8_TYPE_F32) {
-#pragma unroll
-                            for (int q = 0; q < 4; ++q) *reinterpret_cast<float4*>(put(2 * q + hi)) = float4{v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]};
-                        } else if constexpr (kOut == Q8_TYPE_BF16) {
-                            // lanes l and l + 32 hold columns 0-3 and 4-7 of one 8 and of the next, and exchange halves
-#pragma unroll
-                            for (int q = 0; q < 4; q += 2) {
-                                const float* u = v + 4 * q;
-                                const v2u a = __builtin_amdgcn_permlane32_swap(f32_to_bf16x2(u[0], u[1]), f32_to_bf16x2(u[4], u[5]), false, false);
-                                const v2u b = __builtin_amdgcn_permlane32_swap(f32_to_bf16x2(u[2], u[3]), f32_to_bf16x2(u[6], u[7]), false, false);
-                                *reinterpret_cast<v4u*>(put(4 * h + q + hi)) = v4u{a[0], b[0], a[1], b[1]};
-                            }
-                        } else {
-#pragma unroll
-                            for (int q = 0; q < 4; ++q) {
-                                unsigned w = 0;
-#pragma unroll
-                                for (int e = 0; e < 4; ++e) w |= ((unsigned)quantize_code(v[4 * q + e], next_scale) & 0xffu) << (8 * e);
-                                *reinterpret_cast<unsigned*>(put(q / 2) + 8 * (q % 2) + 4 * hi) = w;
-                            }
-                        }
+                        __builtin_amdgcn_raw_buffer_store_b32(code[0] | code[1] << 8 | code[2] << 16 | code[3] << 24, ry, n < N ? row_at + (unsigned)n : kOutOfRange, 0, 0);
                     } else {
 #pragma unroll
-                        for (int e = 0; e < 16; ++e) {
-                            const int m = wm * TM + i * 32 + l32, n = nb + h * 32 + 8 * (e >> 2) + 4 * hi + (e & 3);
-                            const unsigned to = m < tile.rows && n < N ? (unsigned)(m * row_bytes + n * kSize) : kOutOfRange;
-                            if constexpr (kOut == Q8_TYPE_F32)
-                                __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(v[e]), ry, to, 0, 0);
-                            else if constexpr (kOut == Q8_TYPE_BF16)
-                                __builtin_amdgcn_raw_buffer_store_b16(f32_to_bf16(v[e]), ry, to, 0, 0);
-                            else
-                                __builtin_amdgcn_raw_buffer_store_b8((unsigned char)quantize_code(v[e], next_scale), ry, to, 0, 0);
-                        }
+                        for (int e = 0; e < 4; ++e) __builtin_amdgcn_raw_buffer_store_b8((unsigned char)code[e], ry, n + e < N ? row_at + (unsigned)(n + e) : kOutOfRange, 0, 0);
                     }
-                }
-                if (wide) {
-                    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");  // the lanes read what other lanes of this wave wrote
-                    __builtin_amdgcn_wave_barrier();
-#pragma unroll
-                    for (int t = 0; t < 32 * kChunks / 64; ++t) {
-                        const int row = t * (64 / kChunks) + lane / kChunks, c = lane % kChunks, m = wm * TM + i * 32 + row, n = nb + c * (16 / kSize);
-                        const v4u w = *reinterpret_cast<const v4u*>(mine + row * kRowBytes + ((c ^ (row % kChunks)) << 4));
-                        __builtin_amdgcn_raw_buffer_store_b128(w, ry, m < tile.rows && n < N ? (unsigned)(m * row_bytes + n * kSize) : kOutOfRange, 0, 0);
-                    }
-                    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");  // and are done before the next pass writes
-                    __builtin_amdgcn_wave_barrier();
                 }
             }
         }
+    } else {
+        // Rows of a block lie in registers, so a row's place is a scalar offset -- which the bounds check does not see: tiles that are cut short add it to
+        // the lane's own.  bf16: lanes of a pair exchange values of two rows, so that each stores two columns of one, if rows are whole words.
+        const bool odd = lane & 1, words = kOut == Q8_TYPE_BF16 && row_bytes % 4 == 0 && reinterpret_cast<uintptr_t>(p.y) % 4 == 0;
+        const unsigned pick = odd ? 0x07060302u : 0x01000504u;  // v_perm_b32(mine, other): odd {other.high, mine.high}, even {mine.low, other.low}
+        auto store_tile = [&](auto fullc, auto streamc) {
+            constexpr bool kFull = decltype(fullc)::value;
+            constexpr int kAux = decltype(streamc)::value ? 2 : 0;  // aux bit 1: non-temporal
+            auto store = [&](auto value, unsigned at, int row) {
+                const unsigned to = kFull ? at : at + (unsigned)(row * row_bytes);
+                const int uniform = kFull ? row * row_bytes : 0;
+                if constexpr (sizeof(value) == 4)
+                    __builtin_amdgcn_raw_buffer_store_b32(value, ry, to, uniform, kAux);
+                else
+                    __builtin_amdgcn_raw_buffer_store_b16(value, ry, to, uniform, kAux);
+            };
+#pragma unroll
+            for (int j = 0; j < FN; ++j) {
+                const int n = n0 + wn * TN + j * 32 + l32;
+#pragma unroll
+                for (int i = 0; i < FM; ++i) {
+                    float v[16];
+                    block_values(i, j, v);
+                    const int m = wm * TM + i * 32;
+                    const unsigned at = n < N ? (unsigned)(4 * hi * row_bytes + n * kSize) : kOutOfRange;
+                    if constexpr (kOut == Q8_TYPE_F32) {
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) store(__float_as_uint(v[e]), at, m + 8 * (e >> 2) + (e & 3));
+                    } else if (words) {
+                        const unsigned pair_at = n < N ? at + (odd ? (unsigned)row_bytes - 2u : 0u) : kOutOfRange;
+#pragma unroll
+                        for (int e = 0; e < 16; e += 2) {
+                            const unsigned mine = f32_to_bf16x2(v[e], v[e + 1]);
+                            const unsigned other = (unsigned)__builtin_amdgcn_update_dpp(0, (int)mine, 0xB1, 0xf, 0xf, true);  // quad_perm [1, 0, 3, 2]
+                            store(__builtin_amdgcn_perm(mine, other, pick), pair_at, m + 8 * (e >> 2) + (e & 3));
+                        }
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) store(f32_to_bf16(v[e]), at, m + 8 * (e >> 2) + (e & 3));
+                    }
+                }
+            }
+        };
+        if (tile.rows < BM)
+            store_tile(std::false_type{}, std::false_type{});
+        else if (stream_out)
+            store_tile(std::true_type{}, std::true_type{});
+        else
+            store_tile(std::true_type{}, std::false_type{});
     }
     if constexpr (!Op::kMx4)
         if (p.flags & Q8_EPI_ABSMAX) publish_amax<NW>(__float_as_uint(famax), reinterpret_cast<unsigned*>(lds), p.out_amax);
@@ -389,8 +406,11 @@ int launch_product_tile(const Product& p, hipStream_t st)
     if (tiles * WGM * WGN * 64 >= (int64_t)1 << 32) return 1;
     const dim3 grid((unsigned)tiles), block(WGM * WGN * 64);
     const unsigned group_m = 8;
+    // Outputs that the L2s (32 MB together) do not hold anyway are stored past them: 12288 x 1024 -> 4096 to fp32 48.3 us without, 46.9 with; 12288 x 4096 ->
+    // 1024 34.7 and 33.0.
+    const int stream_out = p.M * p.N * (p.y_type == Q8_TYPE_BF16 ? 2 : 4) >= (int64_t)32 << 20;
 #define Q8_PT_LAUNCH(OUT) \
-    hipLaunchKernelGGL((product_tile_kernel<Op, BM, BN, WGM, WGN, kSlots, kAhead, kWgs, OUT>), grid, block, 0, st, p, (unsigned)tiles_n, group_m)
+    hipLaunchKernelGGL((product_tile_kernel<Op, BM, BN, WGM, WGN, kSlots, kAhead, kWgs, OUT>), grid, block, 0, st, p, (unsigned)tiles_n, group_m, stream_out)
     if (p.y_type == Q8_TYPE_F32) {
         Q8_PT_LAUNCH(Q8_TYPE_F32);
     } else if constexpr (Op::kMx4) {

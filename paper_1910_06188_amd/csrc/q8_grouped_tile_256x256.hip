@@ -3,7 +3,7 @@
 
 namespace q8 {
 
-int launch_product_256x256_s2(bool mx4, const Product& p, hipStream_t st)
+int launch_product_256x256(bool mx4, const Product& p, hipStream_t st)
 {
     return mx4 ? launch_product_tile<OpMx4, 256, 256, 2, 4, 2, 2, 1>(p, st) : launch_product_tile<OpI8, 256, 256, 2, 4, 2, 2, 1>(p, st);
 }

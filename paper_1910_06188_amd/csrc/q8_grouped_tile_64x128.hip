@@ -3,7 +3,7 @@
 
 namespace q8 {
 
-int launch_product_64x128_s1(bool mx4, const Product& p, hipStream_t st)
+int launch_product_64x128(bool mx4, const Product& p, hipStream_t st)
 {
     return mx4 ? launch_product_tile<OpMx4, 64, 128, 2, 2, 1, 2, 4>(p, st) : launch_product_tile<OpI8, 64, 128, 2, 2, 1, 2, 4>(p, st);
 }
