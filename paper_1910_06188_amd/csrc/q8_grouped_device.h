@@ -78,46 +78,54 @@ __device__ __forceinline__ GroupPass group_pass(const int32_t* __restrict__ grou
     return q;
 }
 
-// The t-th tile of kRows rows that stay inside a group: its group, its first row of y, its rows (0: there is no such tile).
+// The tiles of kRows rows that stay inside a group: how many there are, and of the t-th its group, its first row of y and its rows (0: there is no
+// such tile).  The first 64 groups are looked at once for both.
 struct RowTile {
     int group, row, rows;
 };
 template <int kRows>
-__device__ __forceinline__ RowTile find_row_tile(const int32_t* __restrict__ group_rows, int n_groups, int M, unsigned t)
-{
-    if (!group_rows) {
-        const int row = (int)(t * kRows);
-        return RowTile{0, row, min(kRows, M - row)};
-    }
-    unsigned before = 0;  // rows of the groups already passed
-    for (int g0 = 0; g0 < n_groups; g0 += 64) {
-        const GroupPass q = group_pass<kRows>(group_rows, n_groups, (unsigned)M, g0, before);
-        const unsigned long long behind = __ballot(t < q.ends);
-        if (behind) {
-            const int l = __builtin_ctzll(behind);
-            const unsigned first = (unsigned)__builtin_amdgcn_readlane((int)(q.ends - q.tiles), l);
-            const int row = __builtin_amdgcn_readlane((int)q.start, l) + (int)((t - first) * kRows);
-            return RowTile{g0 + l, row, min(kRows, __builtin_amdgcn_readlane((int)q.upto, l) - row)};
+struct RowTiles {
+    const int32_t* group_rows;
+    int n_groups;
+    unsigned M, count;
+    GroupPass first;
+    __device__ __forceinline__ explicit RowTiles(const Product& p) : group_rows(p.group_rows), n_groups(p.n_groups), M((unsigned)p.M)
+    {
+        if (!group_rows) {
+            count = (M + kRows - 1) / kRows;
+            return;
         }
-        t -= (unsigned)__builtin_amdgcn_readlane((int)q.ends, 63);
-        before = (unsigned)__builtin_amdgcn_readlane((int)q.upto, 63);
+        first = group_pass<kRows>(group_rows, n_groups, M, 0, 0);
+        count = (unsigned)__builtin_amdgcn_readlane((int)first.ends, 63);
+        unsigned before = (unsigned)__builtin_amdgcn_readlane((int)first.upto, 63);  // rows of the groups already passed
+        for (int g0 = 64; g0 < n_groups; g0 += 64) {
+            const GroupPass q = group_pass<kRows>(group_rows, n_groups, M, g0, before);
+            count += (unsigned)__builtin_amdgcn_readlane((int)q.ends, 63);
+            before = (unsigned)__builtin_amdgcn_readlane((int)q.upto, 63);
+        }
     }
-    return RowTile{0, 0, 0};
-}
-
-// How many such tiles there are.
-template <int kRows>
-__device__ __forceinline__ unsigned count_row_tiles(const int32_t* __restrict__ group_rows, int n_groups, int M)
-{
-    if (!group_rows) return (unsigned)(M + kRows - 1) / kRows;
-    unsigned before = 0, tiles = 0;
-    for (int g0 = 0; g0 < n_groups; g0 += 64) {
-        const GroupPass q = group_pass<kRows>(group_rows, n_groups, (unsigned)M, g0, before);
-        tiles += (unsigned)__builtin_amdgcn_readlane((int)q.ends, 63);
-        before = (unsigned)__builtin_amdgcn_readlane((int)q.upto, 63);
+    __device__ __forceinline__ RowTile find(unsigned t) const
+    {
+        if (!group_rows) {
+            const int row = (int)(t * kRows);
+            return RowTile{0, row, min(kRows, (int)M - row)};
+        }
+        GroupPass q = first;
+        for (int g0 = 0;;) {
+            const unsigned long long behind = __ballot(t < q.ends);
+            if (behind) {
+                const int l = __builtin_ctzll(behind);
+                const unsigned before = (unsigned)__builtin_amdgcn_readlane((int)(q.ends - q.tiles), l);
+                const int row = __builtin_amdgcn_readlane((int)q.start, l) + (int)((t - before) * kRows);
+                return RowTile{g0 + l, row, min(kRows, __builtin_amdgcn_readlane((int)q.upto, l) - row)};
+            }
+            g0 += 64;
+            if (g0 >= n_groups) return RowTile{0, 0, 0};
+            t -= (unsigned)__builtin_amdgcn_readlane((int)q.ends, 63);
+            q = group_pass<kRows>(group_rows, n_groups, M, g0, (unsigned)__builtin_amdgcn_readlane((int)q.upto, 63));
+        }
     }
-    return tiles;
-}
+};
 
 // Tiles of kRows rows that M rows in n_groups groups can have at most: every group that has rows may end inside a tile.
 inline int64_t row_tiles(int64_t M, const int32_t* group_rows, int64_t n_groups, int64_t rows)

@@ -36,7 +36,7 @@ __global__ __launch_bounds__(KW * 64, 4) void product_direct_kernel(Product p, u
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int l32 = lane & 31, hi = lane >> 5, chunk = lane & 7, row8 = lane >> 3;
-    const RowTile tile = find_row_tile<kPdTile>(p.group_rows, p.n_groups, (int)p.M, blockIdx.x % tiles_m);
+    const RowTile tile = RowTiles<kPdTile>(p).find(blockIdx.x % tiles_m);
     if (tile.rows <= 0) return;
     const int64_t n0 = (int64_t)(blockIdx.x / tiles_m) * kPdTile;
     const int pitch = (int)p.pitch;

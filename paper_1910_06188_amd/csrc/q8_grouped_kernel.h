@@ -13,6 +13,7 @@
 
 namespace q8 {
 
+constexpr unsigned kPanel = 8;                 // tile rows of a panel
 constexpr unsigned kOutOfRange = 0x80000000u;  // above the extent of every descriptor here
 
 // 4 bytes per lane from a buffer straight into LDS: lane l lands at lds_addr + 4 l.
@@ -29,7 +30,7 @@ __device__ __forceinline__ void lds_dma4(v4i rsrc, unsigned voff, unsigned lds_a
 //                 lanes', its largest magnitude one exchange away.
 // The bias is what the sums start from.
 template <class Op, int BM, int BN, int WGM, int WGN, int kSlots, int kAhead, int kWgs, int kOut>
-__global__ __launch_bounds__(WGM* WGN * 64, kWgs* WGM* WGN / 4) void product_tile_kernel(Product p, unsigned tiles_n, unsigned group_m, int stream_out)
+__global__ __launch_bounds__(WGM* WGN * 64, kWgs* WGM* WGN / 4) void product_tile_kernel(Product p, unsigned tiles_n, unsigned panel_reciprocal, int stream_out)
 {
 #if defined(__HIP_DEVICE_COMPILE__)
     constexpr bool kRowLane = kOut == Q8_TYPE_MX4 || kOut == Q8_TYPE_I8;
@@ -51,12 +52,22 @@ __global__ __launch_bounds__(WGM* WGN * 64, kWgs* WGM* WGN / 4) void product_til
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const unsigned lds_base = (unsigned)(size_t)(lds_ptr_t)lds;
 
-    // The launch has room for every group ending inside a tile; the tiles that there are go to the XCDs in equal, contiguous shares.
-    const unsigned tiles_m = count_row_tiles<BM>(p.group_rows, p.n_groups, (int)p.M), tiles = tiles_m * tiles_n;
+    // A wave that still has loads to ask for and MFMAs to issue goes before the ones that convert and store.
+    __builtin_amdgcn_s_setprio(3);
+
+    // The launch has room for every group ending inside a tile; the tiles that there are go to the XCDs in equal, contiguous shares, in panels of
+    // kPanel tile rows, column by column.
+    const RowTiles<BM> row_tiles(p);
+    const unsigned tiles_m = row_tiles.count, tiles = tiles_m * tiles_n;
     if (blockIdx.x >= tiles) return;
-    const int pid = tile_of_workgroup(xcd_remap((int)blockIdx.x, (int)tiles), (int)tiles_m, (int)tiles_n, (int)group_m);
-    const RowTile tile = find_row_tile<BM>(p.group_rows, p.n_groups, (int)p.M, (unsigned)pid / tiles_n);
-    const int n0 = (int)((unsigned)pid % tiles_n) * BN;
+    const unsigned pid = (unsigned)xcd_remap((int)blockIdx.x, (int)tiles), per_panel = kPanel * tiles_n;
+    // pid / per_panel by the launch's reciprocal, at most one too small; a division takes as long as a quarter of a stage
+    unsigned panel = (unsigned)(((unsigned long long)pid * panel_reciprocal) >> 32);
+    panel += pid - panel * per_panel >= per_panel;
+    const unsigned in_panel = pid - panel * per_panel, panel_rows = min(kPanel, tiles_m - panel * kPanel);
+    const unsigned col = panel_rows == kPanel ? in_panel / kPanel : in_panel / panel_rows;
+    const RowTile tile = row_tiles.find(panel * kPanel + (in_panel - col * panel_rows));
+    const int n0 = (int)col * BN;
     const int N = (int)p.N, pitch = (int)p.pitch;
     const int last_a = tile.rows - 1, last_b = min(BN, N - n0) - 1;
 
@@ -239,6 +250,8 @@ __global__ __launch_bounds__(WGM* WGN * 64, kWgs* WGM* WGN / 4) void product_til
         multiply(lds, [] {});
     }
 
+    __builtin_amdgcn_s_setprio(0);
+
     // Epilogue.
     typedef unsigned v2u __attribute__((ext_vector_type(2)));
     typedef unsigned v4u __attribute__((ext_vector_type(4)));
@@ -405,12 +418,11 @@ int launch_product_tile(const Product& p, hipStream_t st)
     const int64_t tiles_n = (p.N + BN - 1) / BN, tiles = row_tiles(p.M, p.group_rows, p.n_groups, BM) * tiles_n;
     if (tiles * WGM * WGN * 64 >= (int64_t)1 << 32) return 1;
     const dim3 grid((unsigned)tiles), block(WGM * WGN * 64);
-    const unsigned group_m = 8;
     // Outputs that the L2s (32 MB together) do not hold anyway are stored past them: 12288 x 1024 -> 4096 to fp32 48.3 us without, 46.9 with; 12288 x 4096 ->
     // 1024 34.7 and 33.0.
     const int stream_out = p.M * p.N * (p.y_type == Q8_TYPE_BF16 ? 2 : 4) >= (int64_t)32 << 20;
 #define Q8_PT_LAUNCH(OUT) \
-    hipLaunchKernelGGL((product_tile_kernel<Op, BM, BN, WGM, WGN, kSlots, kAhead, kWgs, OUT>), grid, block, 0, st, p, (unsigned)tiles_n, group_m, stream_out)
+    hipLaunchKernelGGL((product_tile_kernel<Op, BM, BN, WGM, WGN, kSlots, kAhead, kWgs, OUT>), grid, block, 0, st, p, (unsigned)tiles_n, (unsigned)(((int64_t)1 << 32) / (kPanel * tiles_n)), stream_out)
     if (p.y_type == Q8_TYPE_F32) {
         Q8_PT_LAUNCH(Q8_TYPE_F32);
     } else if constexpr (Op::kMx4) {
