@@ -410,14 +410,15 @@ q8_status q8_mx4_fake_quantize(const void* x, int type, int64_t M, int64_t K, vo
  *   y_type Q8_TYPE_MX4: N a multiple of 128; y and y_scales receive the codes and scales of the fp32 result, the same bytes that
  *   q8_mx4_quantize makes of it, and the result itself is not stored: the next layer's quantizer costs no pass over memory.
  *   flags: Q8_EPI_GELU or 0.
- * M, N, K >= 0, K <= Q8_MX4_MAX_K, M * N <= 2^34.
+ * M, N, K >= 0, K <= Q8_MX4_MAX_K; fewer than 2^24 tiles of 32 x 32 outputs (2^34 outputs; of the grouped calls' rows every group's last tile may
+ * be part empty).
  */
 q8_status q8_mx4_linear(const uint8_t* xq, const uint8_t* xs, const uint8_t* wq, const uint8_t* ws, const float* bias, int64_t M,
                         int64_t N, int64_t K, void* y, int y_type, uint8_t* y_scales, uint32_t flags, void* stream);
 
 /*
  * The same on an fp32 or bf16 x [M,K], quantized on the way: the results of q8_mx4_quantize followed by q8_mx4_linear, but for the order in which
- * the fp32 sums are taken.  Two launches, or one for a handful of rows (M <= 32, K <= 4096, M * K <= 32768).
+ * the fp32 sums are taken.  Two launches, or one for few rows (min(M, 32) * K <= 24576, K <= 4096 and at most 512 tiles of 32 x 32 outputs).
  *   xq_work uint8[M * Q8_MX4_CODE_BYTES(K)] (16-byte aligned), xs_work uint8[M * Q8_MX4_SCALE_BYTES(K)] (4-byte aligned): scratch, contents
  *   unspecified on return.
  */
@@ -435,7 +436,7 @@ q8_status q8_mx4_linear_dynamic(const void* x, int x_type, const uint8_t* wq, co
  *   group_rows int32[n_experts], on the device, as q8_route leaves it.  Negative numbers count as zero, and rows beyond M do not exist:
  *   whatever it holds, nothing outside y is written.  Rows of y behind the last group's stay as they are (a buffer may be larger than
  *   the batch), and so do their scales where y holds 4-bit codes.
- *   y, y_type, y_scales, flags as q8_mx4_linear.  1 <= n_experts <= Q8_MAX_EXPERTS; M * N <= 2^34.
+ *   y, y_type, y_scales, flags as q8_mx4_linear.  1 <= n_experts <= Q8_MAX_EXPERTS.
  */
 #define Q8_MAX_EXPERTS 1024
 q8_status q8_mx4_linear_grouped(const uint8_t* xq, const uint8_t* xs, int64_t x_count, const int32_t* x_rows, const uint8_t* wq,

@@ -113,16 +113,16 @@ bool few_tokens_overlap(const float* x, const int8_t* wq, const q8::Epilogue& ep
 bool float_type(int t) { return t == Q8_TYPE_F32 || t == Q8_TYPE_BF16; }
 int64_t type_bytes(int t) { return t == Q8_TYPE_F32 ? 4 : t == Q8_TYPE_BF16 ? 2 : 1; }
 
-constexpr int64_t kMaxOutputs = (int64_t)1 << 34, kMaxRows = 0x7fffffff;
+constexpr int64_t kMaxTiles = (int64_t)1 << 24, kMaxRows = 0x7fffffff;  // a launch is limited to 2^32 threads, a 32x32 tile takes up to 256
 
 // Sizes and pointers that the 4-bit and the int8 products have in common, and what may not overlap.
 q8_status check_product(bool mx4, const q8::Product& p, int64_t K)
 {
     if (p.M < 0 || p.N < 0 || K < 0 || K > (mx4 ? Q8_MX4_MAX_K : Q8_MAX_K) || p.x_count < 0) return Q8_ERR_SHAPE;
     if (p.n_groups < 1 || p.n_groups > Q8_MAX_EXPERTS) return Q8_ERR_SHAPE;
-    if (p.M > kMaxRows || p.N > kMaxRows || p.x_count > kMaxRows || (p.N > 0 && p.M > kMaxOutputs / p.N)) return Q8_ERR_SHAPE;
-    if (p.N > 0 && p.n_groups > kMaxOutputs / p.N) return Q8_ERR_SHAPE;
+    if (p.M > kMaxRows || p.N > kMaxRows || p.x_count > kMaxRows) return Q8_ERR_SHAPE;
     if (p.M == 0 || p.N == 0) return Q8_OK;
+    if (q8::row_tiles(p.M, p.n_groups, 32) * ((p.N + 31) / 32) >= kMaxTiles) return Q8_ERR_SHAPE;
     if (p.x_rows ? p.x_count < 1 : p.x_count != p.M) return Q8_ERR_SHAPE;
     if (!p.y || (K > 0 && (!p.x || !p.w))) return Q8_ERR_NULL;
     if (misaligned(p.x_rows, 4) || misaligned(p.group_rows, 4) || misaligned(p.bias, 4)) return Q8_ERR_ALIGN;
@@ -553,8 +553,9 @@ q8_status q8_route(const float* logits, int64_t T, int n_experts, int k, int32_t
 
 q8_status q8_combine(const void* y, int64_t R, const int32_t* slots, const float* gates, int64_t T, int k, int64_t N, void* out, int type, void* stream)
 {
-    if (R < 0 || T < 0 || N < 0 || k < 1 || R > kMaxRows || T > kMaxRows / k || (N > 0 && (T > kMaxOutputs / N / 8 || R > ((int64_t)1 << 40) / N))) return Q8_ERR_SHAPE;
+    if (R < 0 || T < 0 || N < 0 || k < 1 || R > kMaxRows || T > kMaxRows / k || (N > 0 && R > ((int64_t)1 << 40) / N)) return Q8_ERR_SHAPE;
     if (!float_type(type)) return Q8_ERR_FLAGS;
+    if (N > 0 && T > (((int64_t)1 << 32) - 64) / ((N * type_bytes(type) + 15) / 16)) return Q8_ERR_SHAPE;  // a thread for every 16 bytes of a row
     if (T == 0 || N == 0) return Q8_OK;
     if ((R > 0 && !y) || !slots || !gates || !out) return Q8_ERR_NULL;
     if (misaligned(y, (unsigned)type_bytes(type)) || misaligned(out, (unsigned)type_bytes(type)) || misaligned(slots, 4) || misaligned(gates, 4)) return Q8_ERR_ALIGN;

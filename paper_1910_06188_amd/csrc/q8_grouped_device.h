@@ -127,13 +127,6 @@ struct RowTiles {
     }
 };
 
-// Tiles of kRows rows that M rows in n_groups groups can have at most: every group that has rows may end inside a tile.
-inline int64_t row_tiles(int64_t M, const int32_t* group_rows, int64_t n_groups, int64_t rows)
-{
-    const int64_t ragged = group_rows ? (n_groups < M ? n_groups : M) : 1;
-    return (M + ragged * (rows - 1)) / rows;
-}
-
 // Per-column constants and the value of an output.
 struct ProductColumn {
     int bq;       // int8: quantized bias

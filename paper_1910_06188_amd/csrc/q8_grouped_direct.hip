@@ -143,7 +143,7 @@ __global__ __launch_bounds__(KW * 64, 4) void product_direct_kernel(Product p, u
 template <class Op>
 static int launch(const Product& p, hipStream_t st)
 {
-    const int64_t tm = row_tiles(p.M, p.group_rows, p.n_groups, kPdTile), tiles = tm * ((p.N + kPdTile - 1) / kPdTile);
+    const int64_t tm = row_tiles(p.M, p.n_groups, kPdTile), tiles = tm * ((p.N + kPdTile - 1) / kPdTile);
     if (tiles >= (int64_t)1 << 26) return 1;  // a launch is limited to 2^32 threads
     const dim3 grid((unsigned)tiles);
 #define Q8_PD_LAUNCH(KW) hipLaunchKernelGGL((product_direct_kernel<Op, KW>), grid, dim3(KW * 64), 0, st, p, (unsigned)tm)

@@ -415,7 +415,7 @@ __global__ __launch_bounds__(WGM* WGN * 64, kWgs* WGM* WGN / 4) void product_til
 template <class Op, int BM, int BN, int WGM, int WGN, int kSlots, int kAhead, int kWgs>
 int launch_product_tile(const Product& p, hipStream_t st)
 {
-    const int64_t tiles_n = (p.N + BN - 1) / BN, tiles = row_tiles(p.M, p.group_rows, p.n_groups, BM) * tiles_n;
+    const int64_t tiles_n = (p.N + BN - 1) / BN, tiles = row_tiles(p.M, p.n_groups, BM) * tiles_n;
     if (tiles * WGM * WGN * 64 >= (int64_t)1 << 32) return 1;
     const dim3 grid((unsigned)tiles), block(WGM * WGN * 64);
     // Outputs that the L2s (32 MB together) do not hold anyway are stored past them: 12288 x 1024 -> 4096 to fp32 48.3 us without, 46.9 with; 12288 x 4096 ->

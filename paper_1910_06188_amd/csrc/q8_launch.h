@@ -90,6 +90,8 @@ struct Product {
     int y_type;                  // Q8_TYPE_*
     unsigned flags;
 };
+// Tiles of `rows` rows that M rows in n_groups groups can have at most: every group that has rows may end inside a tile.
+inline int64_t row_tiles(int64_t M, int64_t n_groups, int64_t rows) { return (M + (n_groups < M ? n_groups : M) * (rows - 1)) / rows; }
 // set_product_variant: tuning hook, 0 = automatic.
 void set_product_variant(int v);
 int launch_product(bool mx4, const Product& p, hipStream_t st);

@@ -1,17 +1,18 @@
-// The 4-bit FC layer on an fp32 or bf16 x of at most 32 rows, in one launch: such a layer is bound by launch latency and by how fast the weights come
-// in, and a second launch for the quantizer costs as much again.  Blocks of the format need nothing from outside themselves, so every workgroup quantizes
-// all of x into its own LDS while its first weights are on the way.
+// The 4-bit FC layer on an fp32 or bf16 x of few rows, in one launch: such a layer is bound by launch latency and by how fast the weights come in, and
+// a second launch for the quantizer costs as much again.  Blocks of the format need nothing from outside themselves, so every workgroup quantizes its
+// rows of x into its own LDS while its first weights are on the way.
 //
-//   workgroup = KW waves, one tile of all rows and 32 columns
+//   workgroup = KW waves, one tile of up to 32 rows and 32 columns
 //   wave w    = the 128-byte units w, w + KW, ... of the reduction: four 1 KiB loads of whole lines of w, through LDS of its own
 //
-// 1 x 1024 -> 4096: 10.0 us as two launches, FEW_1 here.
+// As two launches and as one: 1 x 1024 -> 4096 6.2 and 3.6 us, 8 x 1024 -> 4096 6.4 and 4.2, 256 x 512 -> 512 6.6 and 5.1, 128 x 768 -> 768 6.8 and 6.2; from
+// 32 rows of 1024 on two are as fast (6.5 and 7.0), and many tiles slower as one (512 x 1024 -> 1024 7.8 and 10.5).
 #include "q8_grouped_device.h"
 #include "q8_load16.h"
 
 namespace q8 {
 
-constexpr int kFewMaxK = 4096;
+constexpr int kFewMaxK = 4096, kFewElements = 24576, kFewTiles = 512;
 constexpr int kFewRows = 32, kFewUnit = 128, kFewSteps = kFewUnit / 32, kFewUnitBytes = kFewRows * kFewUnit;
 constexpr int kFewRow = kFewRows + 8;  // words of a row of partial sums: the halves of an accumulator store on different banks
 
@@ -33,7 +34,8 @@ __global__ __launch_bounds__(KW * 64, KW / 4) void product_few_kernel(const T* _
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int l32 = lane & 31, hi = lane >> 5, chunk = lane & 7, row8 = lane >> 3;
-    const int pitch = (int)p.pitch, units = (pitch + kFewUnit - 1) / kFewUnit, full = pitch / kFewUnit, groups = pitch / 64, M = (int)p.M;
+    const int pitch = (int)p.pitch, units = (pitch + kFewUnit - 1) / kFewUnit, full = pitch / kFewUnit, groups = pitch / 64;
+    const int row0 = (int)blockIdx.y * kFewRows, rows = (int)min(p.M - row0, (int64_t)kFewRows);
     char* x_scales = lds + kUnits * kFewUnitBytes;
     char* stage = x_scales + kUnits * 2 * kFewRows * 4 + wave * kFewUnitBytes;
     const int64_t n0 = (int64_t)blockIdx.x * 32;
@@ -61,10 +63,10 @@ __global__ __launch_bounds__(KW * 64, KW / 4) void product_few_kernel(const T* _
 
     // Codes and scales of x.  Rows that it does not have stay as they are: their sums go nowhere.
     const unsigned words = (unsigned)pitch / 4;  // of a row's codes
-    for (unsigned i = threadIdx.x; i < words * (unsigned)M; i += KW * 64) {
+    for (unsigned i = threadIdx.x; i < words * (unsigned)rows; i += KW * 64) {
         const unsigned r = i / words, c = i - r * words;
         float v[8];
-        load8(x + (int64_t)r * K + c * 8, (int)max(min(K - (int64_t)c * 8, (int64_t)8), (int64_t)0), v);
+        load8(x + (row0 + (int64_t)r) * K + c * 8, (int)max(min(K - (int64_t)c * 8, (int64_t)8), (int64_t)0), v);
         const unsigned byte = mx4_scale_byte(quad_max_u32(amax8(v)));
         const int at = (int)c * 4;
         *reinterpret_cast<unsigned*>(lds + at / kFewUnit * kFewUnitBytes + r * kFewUnit + (((at % kFewUnit / 16) ^ few_swizzle(r)) << 4) + at % 16) = mx4_codes8(v, byte);
@@ -104,17 +106,21 @@ __global__ __launch_bounds__(KW * 64, KW / 4) void product_few_kernel(const T* _
 #pragma unroll
     for (int e = 0; e < 16; ++e) part[(wave * kFewRows + 8 * (e >> 2) + 4 * hi + (e & 3)) * kFewRow + l32] = acc[e];
     __syncthreads();
-    finish_tile<OpMx4, KW>(p, RowTile{0, 0, M}, n0, part, kFewRow);
+    finish_tile<OpMx4, KW>(p, RowTile{0, row0, rows}, n0, part, kFewRow);
 #endif
 }
 
-// Up to 32 rows whose codes fit LDS beside the rest, and whose quantization in every workgroup costs less than a launch.
-bool mx4_few_eligible(int64_t M, int64_t N, int64_t K) { return M >= 1 && M <= kFewRows && K >= 1 && K <= kFewMaxK && M * K <= 32768 && N <= (int64_t)1 << 20; }
+// Few rows, or few tiles of short ones, whose quantization in every workgroup takes less than a launch.
+bool mx4_few_eligible(int64_t M, int64_t N, int64_t K)
+{
+    const int64_t rows = M < kFewRows ? M : kFewRows, tiles = (M + kFewRows - 1) / kFewRows * ((N + 31) / 32);
+    return M >= 1 && K >= 1 && K <= kFewMaxK && rows * K <= kFewElements && tiles <= kFewTiles;
+}
 
 template <class T>
 static int launch(const T* x, int64_t K, const Product& p, hipStream_t st)
 {
-    const dim3 grid((unsigned)((p.N + 31) / 32));
+    const dim3 grid((unsigned)((p.N + 31) / 32), (unsigned)((p.M + kFewRows - 1) / kFewRows));
     if (p.pitch <= 4 * kFewUnit)
         hipLaunchKernelGGL((product_few_kernel<T, 8, 4>), grid, dim3(512), 0, st, x, K, p);
     else

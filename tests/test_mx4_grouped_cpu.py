@@ -93,6 +93,7 @@ def test_products_refuse(lib):
         for bad in ({"y": x}, {"y": w + 64}, {"y": xs}, {"y": ws}, {"y": b}, {"t": MX4, "ys": x}, {"t": MX4, "ys": y + 64}):
             assert f(**bad) == OVERLAP, bad
         assert f(M=0, x=None, xs=None, w=None, ws=None, y=None) == OK and f(N=0) == OK
+    assert linear(M=1 << 29, N=32) == SHAPE and grouped(M=1 << 14, n=1 << 14, N=1 << 19, E=1024) == SHAPE      # more tiles than a launch takes
     for bad in ({"E": 0}, {"E": 1025}, {"n": 3}, {"n": 0, "rows": r}, {"n": -1}, {"n": 1 << 31, "rows": r}):
         assert grouped(**bad) == SHAPE, bad
     assert grouped(g=None) == NULL
