@@ -494,7 +494,7 @@ void q8_debug_set_gemm_variant(int variant);
 
 /*
  * Forces the kernel behind the 4-bit and grouped products for every later call of this process: 0 = automatic choice (the default),
- * 1 = the 32x32 tiles that take any size and alignment, 2 and up = one tile shape of the staged kernel (what it cannot take goes to 1).
+ * 1 = the 32x32 tiles that take any size and alignment, 2..5 = one tile shape of the staged kernel (what it cannot take goes to 1).
  * An unknown variant makes the products return Q8_ERR_LAUNCH.  Process-global and unsynchronised.
  */
 void q8_debug_set_product_variant(int variant);

@@ -153,7 +153,7 @@ def check_product(y, ref, mag, K, gelu, kind):
     assert (off <= err).all(), (float((off / np.maximum(err, 1e-300)).max()), np.unravel_index((off / np.maximum(err, 1e-300)).argmax(), off.shape))
 
 
-LINEARS = [(1, 1024, 4096), (1, 32, 1), (2, 1, 3), (3, 100, 33), (5, 129, 70), (16, 768, 768), (31, 384, 257), (32, 4096, 64), (33, 640, 96), (64, 256, 2000),
+LINEARS = [(1, 1024, 4096), (1, 32, 1), (2, 1, 3), (3, 3333, 200), (6, 4096, 40), (65, 300, 40), (3, 100, 33), (5, 129, 70), (16, 768, 768), (31, 384, 257), (32, 4096, 64), (33, 640, 96), (64, 256, 2000),
            (129, 2100, 130), (300, 520, 300), (777, 1000, 520), (1500, 256, 384), (2048, 1024, 1024), (515, 4224, 644)]
 
 
@@ -323,6 +323,81 @@ def test_int8_grouped_any_alignment(q8, variant, offset, K):
     assert torch.equal(a[:200].double().cpu(), torch.from_numpy((x[:200].astype(np.int64) @ w[0].astype(np.int64).T).astype(np.float32)).double())
 
 
+def test_grouped_most_experts(q8):
+    """1024 groups, empty, single and longer ones, on both kinds of codes."""
+    g = np.random.default_rng(6)
+    E, N, K = 1024, 128, 128
+    counts = g.integers(0, 4, E).astype(np.int32)
+    counts[[3, 500, 1023]] = 70, 200, 65
+    M, n = int(counts.sum()) + 7, 300
+    rows = g.integers(0, n, M).astype(np.int32)
+    w = dev(tensor(g, E * N, K, 0.5))
+    xq, (wc, ws) = quantized(q8, dev(tensor(g, n, K, 0.5))), quantized(q8, w)
+    ws = ws.view(1, E, N, 4).transpose(0, 1).contiguous()          # [E, G, N, 4] of one group
+    y = torch.full((M, N), 7.0, device="cuda")
+    q8.q8_mx4_linear_grouped(*xq, wc.view(E, N, 64), ws, None, dev(counts), y, x_rows=dev(rows))
+    wv = MX.values(host(wc), host(ws).reshape(1, E * N, 4), K).reshape(E, N, K)
+    ref, mag = MX.grouped(MX.values(host(xq[0]), host(xq[1]), K), wv, None, counts, M, rows)
+    check_product(y[: M - 7], ref[: M - 7], mag[: M - 7], K, False, "f32")
+    assert (y[M - 7:] == 7).all()
+    x8, w8 = g.integers(-127, 128, (n, K)).astype(np.int8), g.integers(-127, 128, (E, N, K)).astype(np.int8)
+    y.fill_(7)
+    q8.q8_linear_grouped(dev(x8), dev(w8), None, torch.ones(1, device="cuda"), torch.ones(E, device="cuda"), dev(counts), y, x_rows=dev(rows))
+    ref, _ = MX.grouped(x8.astype(np.float64), w8.astype(np.float64), None, counts, M, rows)
+    np.testing.assert_array_equal(host(y)[: M - 7], ref[: M - 7])
+    assert (y[M - 7:] == 7).all()
+
+
+@pytest.mark.parametrize("v", [0, 2, 5])
+def test_grouped_rows_of_an_x_beyond_32_bits(q8, v):
+    """Rows picked from the ends of an x of 2.3 GB: what 32-bit offsets cannot reach takes the kernel with 64-bit addresses."""
+    n, K, N = 2250000, 1024, 64
+    x = torch.zeros((n, K), dtype=torch.int8, device="cuda")
+    x[:200], x[-200:] = (torch.randint(-127, 128, (200, K), device="cuda", dtype=torch.int8) for _ in range(2))
+    rows = torch.cat([torch.arange(0, 200), torch.arange(n - 200, n)])[torch.randperm(400)].int().cuda()
+    w = torch.randint(-127, 128, (2, N, K), device="cuda", dtype=torch.int8)
+    y, counts = torch.empty((400, N), device="cuda"), torch.tensor([150, 250], dtype=torch.int32, device="cuda")
+    q8.set_product_variant(v)
+    try:
+        q8.q8_linear_grouped(x, w, None, torch.ones(1, device="cuda"), torch.ones(2, device="cuda"), counts, y, x_rows=rows)
+    finally:
+        q8.set_product_variant(0)
+    mine = x[rows.long()].double()
+    assert torch.equal(y.double(), torch.cat([mine[:150] @ w[0].double().T, mine[150:] @ w[1].double().T]).float().double())
+
+
+@pytest.mark.parametrize("v", [1, 4])
+def test_linear_with_outputs_beyond_32_bits(q8, v):
+    """5.2 GB of outputs: the last rows and columns are where they belong."""
+    M, N, K = 20000, 65536, 128
+    xq, wq = quantized(q8, torch.randn(M, K, device="cuda")), quantized(q8, torch.randn(N, K, device="cuda"))
+    y = torch.full((M, N), float("nan"), device="cuda")
+    q8.set_product_variant(v)
+    try:
+        q8.q8_mx4_linear(*xq, *wq, None, y)
+    finally:
+        q8.set_product_variant(0)
+    xv, wv = (MX.values(host(c[i]), host(s[:, i])) for c, s, i in ((*xq, torch.tensor([0, 1, 9999, 16383, 16384, 16385, 19998, 19999])),
+                                                                    (*wq, torch.tensor([0, 1, 32767, 32768, 65534, 65535]))))
+    got = host(y[[0, 1, 9999, 16383, 16384, 16385, 19998, 19999]][:, [0, 1, 32767, 32768, 65534, 65535]])
+    assert (np.abs(got - xv @ wv.T) <= (K / 64 + 10) * 2.0 ** -23 * (np.abs(xv) @ np.abs(wv).T)).all()
+    assert not y.isnan().any()                        # every output is written (sums of 4-bit products are finite)
+
+
+def test_quantize_a_tensor_beyond_32_bits(q8):
+    """4.4e9 elements: codes and scales of the last rows."""
+    M, K = 2150000, 2048
+    x = torch.zeros((M, K), dtype=torch.bfloat16, device="cuda")
+    x[-40:] = torch.randn(40, K, device="cuda").bfloat16()
+    codes, scales = quantized(q8, x)
+    want_c, want_s = MX.quantize(host(x[-40:]))
+    np.testing.assert_array_equal(host(scales[:, -40:]), want_s)
+    same_codes(host(codes[-40:]), want_c)
+    assert not codes[:-40].any() and not scales[:, :-40].any()
+    q8.q8_mx4_fake_quantize(x, x)
+    np.testing.assert_array_equal(host(x[-40:]), MX.values(want_c, want_s, K))
+
+
 # ---- router and combination ------------------------------------------------------------------------------------------------
 
 def check_route(q8, logits, k):
@@ -436,26 +511,47 @@ class Moe:
         q8.q8_combine(self.y, self.slots, self.gates, self.out, stream=stream)
         return self.out
 
-    def reference(self):
+    def check(self):
+        """Every step against its 64-bit form on what the step before left on the GPU."""
         T, E, k, H, F = self.sizes
+        R = T * k
         experts, gates, counts, rows, slots = MX.route(host(self.logits).astype(np.float32), k)
-        xv = MX.values(*MX.quantize(host(self.x)), H)
+        for got, want in ((self.experts, experts), (self.counts, counts), (self.rows[:R], rows), (self.slots, slots)):
+            np.testing.assert_array_equal(host(got), want)
+        xc, xs = MX.quantize(host(self.x))
+        np.testing.assert_array_equal(host(self.xq[1]), xs)
+        same_codes(host(self.xq[0]), xc)
         vals = lambda w, e, K: MX.values(host(w[0][e]), host(w[1][e]), K)  # noqa: E731
-        h, _ = MX.grouped(xv, [vals(self.w1, e, H) for e in range(E)], host(self.b1), counts, T * k, rows)
-        hv = MX.values(*MX.quantize(MX.gelu(h).astype(np.float32)), F)
-        y, _ = MX.grouped(hv, [vals(self.w2, e, F) for e in range(E)], host(self.b2), counts, T * k)
-        return (gates[..., None] * y[slots]).sum(1)
+        h, mag = MX.grouped(MX.values(xc, xs, H), [vals(self.w1, e, H) for e in range(E)], host(self.b1), counts, R, rows)
+        # The codes of the hidden layer are those of numbers within the product's tolerance of the exact ones; rounding is monotone, so a code's
+        # value lies between the roundings of the ends, in units of the block's scale, which is that of a largest magnitude within the tolerance.
+        ref = MX.gelu(h)
+        err = 1.13 * (H / 64 + 10) * 2.0 ** -23 * mag + 5.2e-7 + 2.0 ** -23 * np.abs(ref)
+        hc, hs = host(self.h[0])[:R], host(self.h[1])[:, :R]
+        byte = hs.transpose(1, 0, 2).reshape(R, F // 32).astype(np.int64)
+        block = lambda a: a.reshape(R, F // 32, 32)  # noqa: E731
+        lo, hi = (np.maximum(np.frexp(np.maximum(np.abs(block(ref)) + d * block(err), 0).max(-1))[1] - 3, -127) + 127 for d in (-1, 1))
+        assert ((byte >= lo) & (byte <= hi)).all()
+        unit = np.repeat(np.ldexp(1.0, byte - 127), 32, 1)
+        hv = MX.values(hc, hs, F)
+        code = lambda v: np.sign(v) * MX.GRID[np.abs(np.minimum(np.abs(v), 6)[..., None] - MX.GRID).argmin(-1)]  # noqa: E731
+        step = 1e-9                                   # a tie may go either way here
+        assert (hv / unit >= code((ref - err) / unit * (1 - step * np.sign(ref - err)))).all()
+        assert (hv / unit <= code((ref + err) / unit * (1 + step * np.sign(ref + err)))).all()
+        y, mag = MX.grouped(hv, [vals(self.w2, e, F) for e in range(E)], host(self.b2), counts, R)
+        check_product(self.y[:R], y, mag, F, False, "bf16")
+        got_y, got_g = host(self.y), host(self.gates)
+        terms = got_g[..., None] * got_y[slots]
+        out, mag = terms.sum(1), np.abs(terms).sum(1)
+        err = k * 2.0 ** -24 * 1.001 * mag
+        assert (np.abs(host(self.out) - out) <= err + 2.0 ** -8 * (np.abs(out) + err)).all()
 
 
 @pytest.mark.parametrize("T,E,k,H,F,room", [(1, 4, 2, 128, 256, 0), (33, 8, 2, 200, 384, 5), (700, 6, 3, 256, 512, 40), (3000, 2, 1, 256, 256, 0)])
 def test_mixture_of_experts(q8, T, E, k, H, F, room):
     m = Moe(q8, T, E, k, H, F, room)
-    got, ref = host(m.run()), m.reference()
-    # y and the sum are each rounded to bf16 (2^-8 each of values up to the largest); a code of the hidden layer that lies on a
-    # rounding border may fall on either side, which moves an output by a code's step times a weight: of F of them one or two
-    scale = np.abs(ref).max()
-    assert np.abs(got - ref).max() <= 3 * 2.0 ** -8 * scale + 0.02 * scale
-    assert np.linalg.norm(got - ref) <= 2.0 ** -7 * np.linalg.norm(ref)
+    m.run()
+    m.check()
 
 
 def test_mixture_of_experts_captured_and_replayed(q8):
