@@ -69,35 +69,54 @@ __global__ __launch_bounds__(WGM* WGN * 64, kWgs* WGM* WGN / 4) void product_til
     const RowTile tile = row_tiles.find(panel * kPanel + (in_panel - col * panel_rows));
     const int n0 = (int)col * BN;
     const int N = (int)p.N, pitch = (int)p.pitch;
-    const int last_a = tile.rows - 1, last_b = min(BN, N - n0) - 1;
+    const int rows_b = min(BN, N - n0);
 
-    // Row of the x descriptor for the tile's row r: its place among the tile's rows, or in the whole of x.
-    const auto x_row = [&](int r) -> int {
-        const int m = min(r, last_a);
-        if (!p.x_rows) return m;
-        const int id = p.x_rows[tile.row + m];
-        return id >= 0 && id < (int)p.x_count ? id : -1;
-    };
+    // Offsets of this lane's 16 bytes in the operands' descriptors, of whose rows it loads every eighth; rows behind the tile's are out of range, which takes no
+    // comparison: a row's offset is at least its number times the pitch.  x starts at the tile's first row, or, where rows are picked by index, at its own.
     const int64_t x_first = p.x_rows ? 0 : tile.row;
     const unsigned x_extent = p.x_rows ? (unsigned)p.x_count : (unsigned)tile.rows;
     const uint8_t* Xt = p.x + x_first * pitch;
     const uint8_t* Wt = p.w + ((int64_t)tile.group * N + n0) * pitch;
-    unsigned a_off[A_LOADS], b_off[B_LOADS];
     const int chunk = lane & 7, row8 = lane >> 3;
-#pragma unroll
-    for (int i = 0; i < A_LOADS; ++i) {
-        const int r = (wave * A_LOADS + i) * 8 + row8, id = x_row(r);
-        a_off[i] = id < 0 ? kOutOfRange : (unsigned)id * (unsigned)pitch + (unsigned)((chunk ^ swizzle_of_row(r)) * 16);
-    }
-#pragma unroll
-    for (int i = 0; i < B_LOADS; ++i) {
-        const int r = (wave * B_LOADS + i) * 8 + row8;
-        b_off[i] = (unsigned)min(r, last_b) * (unsigned)pitch + (unsigned)((chunk ^ swizzle_of_row(r)) * 16);
-    }
-    // The scale loads of this wave, 64 rows of one group of a stage each: the words of its group in the first stage, from one stage to the
-    // next, and how far they go.
+    // swizzle_of_row(r) of row r = 8 g + row8 is row8 ^ g, three bits of each
+    const auto chunk_at = [&](int g) { return (unsigned)(((chunk ^ row8) << 4) ^ ((g & 7) << 4)); };
+    unsigned a_off[A_LOADS], b_off[B_LOADS];
     const int groups = pitch / 64;
     unsigned s_off[S_LOADS ? S_LOADS : 1];
+#pragma unroll
+    for (int i = 0; i < B_LOADS; ++i) {
+        const int g = wave * B_LOADS + i;
+        b_off[i] = (unsigned)row8 * (unsigned)pitch + (unsigned)(g * 8 * pitch) + chunk_at(g);
+    }
+    // The scale loads of this wave, 64 rows of one group of a stage each.
+    const auto scale_row = [&](int i) {  // row of the operand that load i takes to this lane
+        const int u = wave + i * NW;
+        return u < BM / 32 ? u % (BM / 64) * 64 + lane : (u - BM / 32) % (BN / 64) * 64 + lane;
+    };
+    if (p.x_rows) {
+        int id[A_LOADS], scale_id[S_LOADS ? S_LOADS : 1];  // all asked for before the first is looked at
+#pragma unroll
+        for (int i = 0; i < A_LOADS; ++i) id[i] = p.x_rows[tile.row + min((wave * A_LOADS + i) * 8 + row8, tile.rows - 1)];
+#pragma unroll
+        for (int i = 0; i < S_LOADS; ++i) scale_id[i] = p.x_rows[tile.row + min(scale_row(i), tile.rows - 1)];
+#pragma unroll
+        for (int i = 0; i < A_LOADS; ++i)
+            a_off[i] = (unsigned)id[i] < (unsigned)p.x_count ? (unsigned)id[i] * (unsigned)pitch + chunk_at(wave * A_LOADS + i) : kOutOfRange;
+#pragma unroll
+        for (int i = 0; i < S_LOADS; ++i) {
+            const bool there = (unsigned)scale_id[i] < (unsigned)p.x_count;
+            s_off[i] = wave + i * NW >= BM / 32 ? (unsigned)scale_row(i) * 4u : there ? (unsigned)scale_id[i] * 4u : kOutOfRange;
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < A_LOADS; ++i) {
+            const int g = wave * A_LOADS + i;
+            a_off[i] = (unsigned)row8 * (unsigned)pitch + (unsigned)(g * 8 * pitch) + chunk_at(g);
+        }
+#pragma unroll
+        for (int i = 0; i < S_LOADS; ++i) s_off[i] = (unsigned)scale_row(i) * 4u;
+    }
+    // Of each scale load: the words of its group in the first stage, from one stage to the next, how far they go, which group of the stage.
     const uint8_t* s_base[S_LOADS ? S_LOADS : 1];
     int64_t s_step[S_LOADS ? S_LOADS : 1];
     unsigned s_extent[S_LOADS ? S_LOADS : 1];
@@ -107,20 +126,17 @@ __global__ __launch_bounds__(WGM* WGN * 64, kWgs* WGM* WGN / 4) void product_til
         for (int i = 0; i < S_LOADS; ++i) {
             const int u = wave + i * NW;
             const bool of_x = u < BM / 32;
-            const int v = of_x ? u : u - BM / 32, per = of_x ? BM / 64 : BN / 64;
-            const int r = v % per * 64 + lane, id = of_x ? x_row(r) : min(r, last_b);
-            s_off[i] = id < 0 ? kOutOfRange : (unsigned)id * 4u;
-            s_group[i] = v / per;
+            s_group[i] = of_x ? u / (BM / 64) : (u - BM / 32) / (BN / 64);
             const int64_t rows = of_x ? p.x_count : (int64_t)N;
             const uint8_t* all = of_x ? p.xs + x_first * 4 : p.ws + ((int64_t)tile.group * groups * N + n0) * 4;
             s_base[i] = all + s_group[i] * rows * 4;
             s_step[i] = rows * 8;
-            s_extent[i] = (of_x ? x_extent : (unsigned)(last_b + 1)) * 4u;
+            s_extent[i] = (of_x ? x_extent : (unsigned)rows_b) * 4u;
         }
     }
 
     const int KT = pitch / kBK, tail = pitch % kBK;  // whole stages, and the bytes behind them (a whole number of 16)
-    const unsigned extent_a = x_extent * (unsigned)pitch, extent_b = (unsigned)(last_b + 1) * (unsigned)pitch;
+    const unsigned extent_a = x_extent * (unsigned)pitch, extent_b = (unsigned)rows_b * (unsigned)pitch;
     // Stage kt into a slot; past the end of the rows through empty descriptors, which fetch nothing.
     auto load_stage = [&](int kt, int slot, auto whole) {
         constexpr bool kWhole = decltype(whole)::value;
@@ -359,9 +375,12 @@ __global__ __launch_bounds__(WGM* WGN * 64, kWgs* WGM* WGN / 4) void product_til
         }
     } else {
         // Rows of a block lie in registers, so a row's place is a scalar offset -- which the bounds check does not see: tiles that are cut short add it to
-        // the lane's own.  bf16: lanes of a pair exchange values of two rows, so that each stores two columns of one, if rows are whole words.
-        const bool odd = lane & 1, words = kOut == Q8_TYPE_BF16 && row_bytes % 4 == 0 && reinterpret_cast<uintptr_t>(p.y) % 4 == 0;
-        const unsigned pick = odd ? 0x07060302u : 0x01000504u;  // v_perm_b32(mine, other): odd {other.high, mine.high}, even {mine.low, other.low}
+        // the lane's own.  bf16, if rows are whole words: two blocks beside each other have 64 columns, a line of a row.  The even lanes store two neighbours of the
+        // first, the odd ones of the second, for one row and then for the next (a block by itself would store half lines of two rows at once, which took
+        // 40 cycles an instruction against 17).
+        const bool odd = lane & 1, words = kOut == Q8_TYPE_BF16 && FN % 2 == 0 && row_bytes % 4 == 0 && reinterpret_cast<uintptr_t>(p.y) % 4 == 0;
+        // v_perm_b32(mine, other): the low halves, the lower lane's first, and the high halves
+        const unsigned low = odd ? 0x05040100u : 0x01000504u, high = odd ? 0x07060302u : 0x03020706u;
         auto store_tile = [&](auto fullc, auto streamc) {
             constexpr bool kFull = decltype(fullc)::value;
             constexpr int kAux = decltype(streamc)::value ? 2 : 0;  // aux bit 1: non-temporal
@@ -376,26 +395,37 @@ __global__ __launch_bounds__(WGM* WGN * 64, kWgs* WGM* WGN / 4) void product_til
 #pragma unroll
             for (int j = 0; j < FN; ++j) {
                 const int n = n0 + wn * TN + j * 32 + l32;
+                const unsigned at = n < N ? (unsigned)(4 * hi * row_bytes + n * kSize) : kOutOfRange;
 #pragma unroll
                 for (int i = 0; i < FM; ++i) {
-                    float v[16];
-                    block_values(i, j, v);
                     const int m = wm * TM + i * 32;
-                    const unsigned at = n < N ? (unsigned)(4 * hi * row_bytes + n * kSize) : kOutOfRange;
-                    if constexpr (kOut == Q8_TYPE_F32) {
+                    if (words) {
+                        if constexpr (kOut == Q8_TYPE_BF16 && FN % 2 == 0) {
+                            if (j % 2) continue;
+                            float v[16], w[16];
+                            block_values(i, j, v);
+                            block_values(i, j + 1, w);
+                            const int pair = n0 + wn * TN + j * 32 + (odd ? 32 + l32 - 1 : l32);
+                            const unsigned pair_at = pair < N ? (unsigned)(4 * hi * row_bytes + pair * 2) : kOutOfRange;
 #pragma unroll
-                        for (int e = 0; e < 16; ++e) store(__float_as_uint(v[e]), at, m + 8 * (e >> 2) + (e & 3));
-                    } else if (words) {
-                        const unsigned pair_at = n < N ? at + (odd ? (unsigned)row_bytes - 2u : 0u) : kOutOfRange;
-#pragma unroll
-                        for (int e = 0; e < 16; e += 2) {
-                            const unsigned mine = f32_to_bf16x2(v[e], v[e + 1]);
-                            const unsigned other = (unsigned)__builtin_amdgcn_update_dpp(0, (int)mine, 0xB1, 0xf, 0xf, true);  // quad_perm [1, 0, 3, 2]
-                            store(__builtin_amdgcn_perm(mine, other, pick), pair_at, m + 8 * (e >> 2) + (e & 3));
+                            for (int e = 0; e < 16; e += 2) {
+                                const unsigned a = f32_to_bf16x2(v[e], v[e + 1]), b = f32_to_bf16x2(w[e], w[e + 1]);
+                                const unsigned mine = odd ? b : a;
+                                const unsigned other = (unsigned)__builtin_amdgcn_update_dpp(0, (int)(odd ? a : b), 0xB1, 0xf, 0xf, true);  // quad_perm [1, 0, 3, 2]
+                                store(__builtin_amdgcn_perm(mine, other, low), pair_at, m + 8 * (e >> 2) + (e & 3));
+                                store(__builtin_amdgcn_perm(mine, other, high), pair_at, m + 8 * (e >> 2) + (e & 3) + 1);
+                            }
                         }
                     } else {
+                        float v[16];
+                        block_values(i, j, v);
 #pragma unroll
-                        for (int e = 0; e < 16; ++e) store(f32_to_bf16(v[e]), at, m + 8 * (e >> 2) + (e & 3));
+                        for (int e = 0; e < 16; ++e) {
+                            if constexpr (kOut == Q8_TYPE_F32)
+                                store(__float_as_uint(v[e]), at, m + 8 * (e >> 2) + (e & 3));
+                            else
+                                store(f32_to_bf16(v[e]), at, m + 8 * (e >> 2) + (e & 3));
+                        }
                     }
                 }
             }
