@@ -4,6 +4,7 @@
 //   y[r,n] = act( sum_k x[rows[r],k] w[g(r),n,k] + bias[g(r),n] )        g(r) the group of row r
 //
 // This file holds the choice of the kernel.
+#include "q8.h"
 #include "q8_launch.h"
 
 namespace q8 {
@@ -35,32 +36,38 @@ static bool tile_eligible(const Product& p, int64_t rows)
 }
 
 // The kernel of a launch, by sizes alone: sums of a tiled kernel do not depend on its tile, so that outputs of every type are the same sums.
-//   1 (32x32, the reduction dealt out over the waves) while tiles are few: up to 256 for short rows (1 x 1024 -> 4096 on 4-bit codes 3.8 us, 64x64 tiles 4.6;
-//     300 x 520 -> 1000, 320 tiles, 6.0 and 4.5), up to 1024 for rows of 2 KiB and more, whose serial walk a larger tile cannot hide (64 x 4096 -> 1024 5.3 and
-//     8.4; int8, 200 rows of 8 experts, 4096 -> 1024 12.8 and 20.0).
-//   2 (64x64) for groups of few rows each, which leave most of a larger tile empty (64 rows of 64 experts, 1024 -> 4096 15.9 us, 64x128 17.7, 128x128 20.6).
-//   5 (256x256) for long rows once every unit has a tile: it asks LDS for the least (4096^3 to bf16 41.5 us, 128x128 47.0; but 12288 x 4096 -> 1024, 192 tiles,
-//     37.9 and 32.0).
-//   4 (128x128) from three tiles a unit on, two for long rows (12288 x 1024 -> 4096 to bf16 49 us, 64x128 60; 2048 x 1024 -> 4096, two tiles a unit, 13.2
-//     and 11.1), unless groups are so small that the rows left over count for more (128 rows a group, 1024 -> 2048: 37.0 and 29.6).
-//   3 (64x128) in between, and 2 again where those are fewer than two a unit (2048 x 1024 -> 1024 6.5 us, 64x128 7.1).
-static int choose(const Product& p)
+// Long rows are those of 2 KiB of codes and more; times in us, the alternatives taken in turn.
+//   1 (32x32, the reduction dealt out over the waves) up to 256 tiles (300 x 520 -> 1000, 320 of them, 5.5, 64x64 4.2), and up to 512 of long rows, whose serial
+//     walk a larger tile cannot hide (64 x 4096 -> 1024 4.7 and 7.6; int8, 275 rows of 16 experts, 4096 -> 512 9.5 and 19.7; but 754 rows of 8 experts, 2048 ->
+//     1024, about 900, 14.6 and 9.1).
+//   2 or 3 for groups of few rows each, which leave most of a larger tile empty (4809 rows of 64 experts, 768 -> 2048 17.2 and 17.8, 128x128 20.9).
+//   5 (256x256) for long rows whose tiles leave less than a quarter of a round of the 256 units idle: it moves the fewest operand bytes, but a unit holds one at
+//     a time and waits for the last round (4096 -> 1024: 14336 rows, 224 tiles, 35.5 and 128x128 42.7; 12288 rows, 192, 36.3 and 32.9; 28672 rows, 448, 67.6 and
+//     68.6; 24576 rows, 384, 65.9 and 57.8).  int8 rows have to be 8 KiB (16384 x 8192 -> 1024 117 and 129; 8192 x 4096 -> 4096 138 and 130).
+//     Short rows to 4-bit codes, whose epilogue is bound by arithmetic, if it is one round (3997 x 1024 -> 4096 12.2 and 14.6).
+//   4 (128x128) from two tiles a unit on (2184 x 1024 -> 4096 10.4 and 64x128 11.2; 12288 x 1024 -> 4096 to fp32 47 and 51), of long rows from one and a half
+//     (6396 x 4096 -> 1024 20.0 and 24.4), for int8, whose MFMAs take twice as long, also in groups that are a tile each (15373 rows of 128 experts, 512 -> 2048
+//     49.8 and 52.7; on 4-bit codes 16145 rows, 768 -> 4096 99.9 and 92.6).
+//   3 (64x128) against 2 (64x64): from two tiles a unit on (8192 rows of 16 experts, 512 -> 4096 24.5 and 32.4), unless rows are short and groups small; and for
+//     short rows to 4-bit codes, of which its waves store 16 bytes a lane and the other's 8 (5330 rows of 64 experts, 1024 -> 512 6.6 and 7.7).
+static int choose(bool mx4, const Product& p)
 {
     const int64_t groups = p.group_rows ? (p.n_groups < p.M ? p.n_groups : p.M) : 0;  // of which half a tile each is left over
     const auto tiles = [&](int64_t rows, int64_t cols) { return ((p.M + rows - 1) / rows + groups / 2) * ((p.N + cols - 1) / cols); };
-    const bool is_long = p.pitch >= 2048;
-    if (tiles(32, 32) <= 256 || (is_long && tiles(32, 32) <= 1024)) return 1;
-    if (p.M < 96 * groups) return 2;
-    if (is_long && tiles(256, 256) >= 256) return 5;
-    if (p.M > 160 * groups && tiles(128, 128) >= (is_long ? 512 : 768)) return 4;
-    return tiles(64, 128) >= 512 ? 3 : 2;
+    const bool is_long = p.pitch >= 2048, small = p.M < 96 * groups;
+    if (tiles(32, 32) <= (is_long ? 512 : 256)) return 1;
+    const int64_t largest = tiles(256, 256), idle = -largest & 255;
+    if (!small && idle < 64 && (p.pitch >= (mx4 ? 2048 : 8192) || (p.y_type == Q8_TYPE_MX4 && largest <= 256))) return 5;
+    if (!small && (!mx4 || p.M > 160 * groups) && tiles(128, 128) >= (is_long ? 384 : 512)) return 4;
+    if (!is_long && p.y_type == Q8_TYPE_MX4) return 3;
+    return tiles(64, 128) >= 512 && (is_long || !small) ? 3 : 2;
 }
 
 int launch_product(bool mx4, const Product& p, hipStream_t st)
 {
     int v = g_variant;
     if (v < 0 || v > 1 + (int)(sizeof(kTiles) / sizeof(kTiles[0]))) return 1;
-    if (v == 0) v = choose(p);
+    if (v == 0) v = choose(mx4, p);
     if (v > 1 && tile_eligible(p, kTiles[v - 2].rows)) return kTiles[v - 2].launch(mx4, p, st);
     return launch_product_direct(mx4, p, st);
 }

@@ -25,7 +25,7 @@ __device__ __forceinline__ void lds_dma4(v4i rsrc, unsigned voff, unsigned lds_a
 // kOut: the type of y.  It decides which operand the MFMA takes first, that is, what a lane holds of a 32x32 block.
 //   fp32, bf16    x first: one column and 16 rows.  32 lanes store 32 neighbours of a row at once, whole 128-byte lines of fp32.  (With a row and 16
 //                 columns a lane, stores take 16 bytes a lane but 32 bytes of 32 rows each, four times the requests to the L2: 12288 x 1024 -> 4096 to fp32
-//                 59 us against 48; through LDS to whole lines 56, because LDS is what the MFMAs wait for.)
+//                 59 us against 48; through LDS to whole lines 56; two columns of every other row a lane, exchanged in pairs, 50 against 45.)
 //   4-bit, int8   w first: one row and four times four neighbouring columns.  A block of the 4-bit format -- 32 neighbours of a row -- is two
 //                 lanes', its largest magnitude one exchange away.
 // The bias is what the sums start from.
@@ -376,8 +376,8 @@ __global__ __launch_bounds__(WGM* WGN * 64, kWgs* WGM* WGN / 4) void product_til
     } else {
         // Rows of a block lie in registers, so a row's place is a scalar offset -- which the bounds check does not see: tiles that are cut short add it to
         // the lane's own.  bf16, if rows are whole words: two blocks beside each other have 64 columns, a line of a row.  The even lanes store two neighbours of the
-        // first, the odd ones of the second, for one row and then for the next (a block by itself would store half lines of two rows at once, which took
-        // 40 cycles an instruction against 17).
+        // first, the odd ones of the second, for one row and then for the next (a block by itself would store half lines of two rows at once: 24576 rows of 16
+        // experts, 1024 -> 4096 85.6 us against 82.7, 12288 rows without groups 42.2 against 41).
         const bool odd = lane & 1, words = kOut == Q8_TYPE_BF16 && FN % 2 == 0 && row_bytes % 4 == 0 && reinterpret_cast<uintptr_t>(p.y) % 4 == 0;
         // v_perm_b32(mine, other): the low halves, the lower lane's first, and the high halves
         const unsigned low = odd ? 0x05040100u : 0x01000504u, high = odd ? 0x07060302u : 0x03020706u;
@@ -448,8 +448,8 @@ int launch_product_tile(const Product& p, hipStream_t st)
     const int64_t tiles_n = (p.N + BN - 1) / BN, tiles = row_tiles(p.M, p.n_groups, BM) * tiles_n;
     if (tiles * WGM * WGN * 64 >= (int64_t)1 << 32) return 1;
     const dim3 grid((unsigned)tiles), block(WGM * WGN * 64);
-    // Outputs that the L2s (32 MB together) do not hold anyway are stored past them: 12288 x 1024 -> 4096 to fp32 48.3 us without, 46.9 with; 12288 x 4096 ->
-    // 1024 34.7 and 33.0.
+    // Outputs that the L2s (32 MB together) do not hold anyway are stored past them: 12288 x 4096 -> 1024 to fp32 33.4 us without, 31.9 with; 12288 x 1024 -> 4096 to
+    // bf16 42.6 and 41.0, to fp32 47.0 and 48.2.
     const int stream_out = p.M * p.N * (p.y_type == Q8_TYPE_BF16 ? 2 : 4) >= (int64_t)32 << 20;
 #define Q8_PT_LAUNCH(OUT) \
     hipLaunchKernelGGL((product_tile_kernel<Op, BM, BN, WGM, WGN, kSlots, kAhead, kWgs, OUT>), grid, block, 0, st, p, (unsigned)tiles_n, (unsigned)(((int64_t)1 << 32) / (kPanel * tiles_n)), stream_out)
