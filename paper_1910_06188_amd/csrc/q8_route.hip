@@ -4,7 +4,7 @@
 // The sort is a counting sort in two launches.  Tokens are cut into at most kBlocks runs.  The first launch picks the experts, 16 lanes
 // a token, and counts each run's pairs of every expert.  The second adds up, for each run, the pairs that precede it -- those of smaller
 // experts and those of earlier runs -- and places its own in order.  Only whole numbers are added, so no order of workgroups or atomics
-// changes a result.  Batches of one run take both steps in one launch.
+// changes a result.  Small batches take both steps in one launch.  (12288 tokens, 2 of 64 experts: 3.8 and 6.0 us, chains of latencies.)
 #include <float.h>
 
 #include "q8_grouped_device.h"
@@ -12,7 +12,7 @@
 namespace q8 {
 
 constexpr int kRouteBlocks = Q8_ROUTE_BLOCKS, kRouteThreads = 1024, kRouteWaves = kRouteThreads / 64, kRouteExperts = Q8_ROUTE_MAX_EXPERTS;
-constexpr int kRouteLeast = kRouteThreads / 16;  // tokens of a run at least: a pass of a workgroup
+constexpr int kRouteSinglePairs = 512;  // of a batch that one workgroup takes
 
 // Unsigned order of floats: -inf < ... < -0 < +0 < ... < +inf.  NaN counts as -inf.  +0 and -0 are the same logit.
 __device__ __forceinline__ unsigned logit_key(float f)
@@ -23,57 +23,117 @@ __device__ __forceinline__ unsigned logit_key(float f)
 }
 __device__ __forceinline__ float logit_of_key(unsigned k) { return __uint_as_float(k ^ (k >> 31 ? 0x80000000u : 0xffffffffu)); }
 
+// A logit and its index as one number: 2^52 + 2^10 key + 1023 - index, an exact double, so that the larger of two is one instruction and of equal logits the
+// lower index is the larger number.  0 is below all of them.
+constexpr int kIndexBits = 10;
+static_assert(kRouteExperts <= 1 << kIndexBits, "an index has ten bits");
+__device__ __forceinline__ double candidate(float logit, int index, bool there)
+{
+    const unsigned key = logit_key(logit), mask = 0u - (unsigned)there;  // 0 where there is no such logit
+    return __hiloint2double((int)((0x43300000u | key >> (32 - kIndexBits)) & mask), (int)((key << kIndexBits | (unsigned)((1 << kIndexBits) - 1 - index)) & mask));
+}
+__device__ __forceinline__ float logit_of(double c)
+{
+    return logit_of_key((unsigned)__double2hiint(c) << (32 - kIndexBits) | (unsigned)__double2loint(c) >> kIndexBits);
+}
+__device__ __forceinline__ int index_of(double c) { return (1 << kIndexBits) - 1 - (__double2loint(c) & ((1 << kIndexBits) - 1)); }
+
 // Over the 16 lanes of a row, the same value in every lane.
 template <int kCtrl>
-__device__ __forceinline__ unsigned ror(unsigned v)
+__device__ __forceinline__ int ror(int v)
 {
-    return (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, 0x120 + kCtrl, 0xf, 0xf, true);
+    return __builtin_amdgcn_update_dpp(0, v, 0x120 + kCtrl, 0xf, 0xf, true);
 }
-__device__ __forceinline__ unsigned row_max_u32(unsigned v)
+template <int kCtrl>
+__device__ __forceinline__ double max_ror(double v)
 {
-    v = max(v, ror<8>(v));
-    v = max(v, ror<4>(v));
-    v = max(v, ror<2>(v));
-    return max(v, ror<1>(v));
+    return __builtin_fmax(v, __hiloint2double(ror<kCtrl>(__double2hiint(v)), ror<kCtrl>(__double2loint(v))));
 }
-__device__ __forceinline__ unsigned row_min_u32(unsigned v)
+__device__ __forceinline__ double row_max(double v) { return max_ror<1>(max_ror<2>(max_ror<4>(max_ror<8>(v)))); }
+template <int kCtrl>
+__device__ __forceinline__ float add_ror(float v)
 {
-    v = min(v, ror<8>(v));
-    v = min(v, ror<4>(v));
-    v = min(v, ror<2>(v));
-    return min(v, ror<1>(v));
+    return v + __int_as_float(ror<kCtrl>(__float_as_int(v)));
+}
+__device__ __forceinline__ float row_sum(float v) { return add_ror<1>(add_ror<2>(add_ror<4>(add_ror<8>(v)))); }
+
+__device__ __forceinline__ void exchange(double& a, double& b)
+{
+    const double large = __builtin_fmax(a, b);
+    b = __builtin_fmin(a, b);
+    a = large;
+}
+// c[0 .. n) from "falling, then rising" to falling.
+template <int n>
+__device__ __forceinline__ void merge_falling(double* c)
+{
+#pragma unroll
+    for (int d = n / 2; d > 0; d /= 2)
+#pragma unroll
+        for (int i = 0; i < n; ++i)
+            if (!(i & d)) exchange(c[i], c[i + d]);
+}
+// c[0 .. n) in falling order: halves sorted, the largest of the one against the smallest of the other, and either side merged.
+template <int n>
+__device__ __forceinline__ void sort_falling(double* c)
+{
+    if constexpr (n > 1) {
+        sort_falling<n / 2>(c);
+        sort_falling<n / 2>(c + n / 2);
+#pragma unroll
+        for (int i = 0; i < n / 2; ++i) exchange(c[i], c[n - 1 - i]);
+        merge_falling<n / 2>(c);
+        merge_falling<n / 2>(c + n / 2);
+    }
 }
 
-// The k experts of a token by 16 lanes, four tokens a wave: lane r of them holds the logits (raw) r*kPer .. r*kPer + kPer - 1.  Every round takes
-// the largest key left over (0 is below all of them) and, of several, the lowest index.  Lane j returns choice j.
+// The k experts of a token by 16 lanes, four tokens a wave.  Lane r of them takes the logits r, r + 16, ... , kPer of them, as falling lists of four; or, beyond 16 of them,
+// in batches of 16 of which it keeps the largest 16, one list, and k is no more.  Every round takes the largest head of all lists and moves its list on.
 template <int kPer>
-__device__ __forceinline__ void choose(const float* raw, int n_experts, int k, int& expert, float& gate)
+__device__ __forceinline__ void choose(const float* __restrict__ logits, int n_experts, int k, int& expert, float& gate)
 {
+    constexpr int kHeld = kPer < 16 ? kPer : 16, kList = kPer > kHeld ? kHeld : 4;
     const int r = threadIdx.x & 15, row = threadIdx.x & 48;
-    unsigned key[kPer];
+    double held[kHeld];
+#pragma unroll 1
+    for (int b = 0; b < kPer; b += kHeld) {
+        float raw[kHeld];
+        double c[kHeld];
 #pragma unroll
-    for (int i = 0; i < kPer; ++i) key[i] = r * kPer + i < n_experts ? logit_key(raw[i]) : 0u;
-    unsigned chosen = 0;
-    expert = 0;
+        for (int i = 0; i < kHeld; ++i) raw[i] = logits[min((b + i) * 16 + r, n_experts - 1)];
+#pragma unroll
+        for (int i = 0; i < kHeld; ++i) asm volatile("" : "+v"(raw[i]));  // all under way before the first is looked at, and no branch around any
+#pragma unroll
+        for (int i = 0; i < kHeld; ++i) c[i] = candidate(raw[i], (b + i) * 16 + r, (b + i) * 16 + r < n_experts);
+#pragma unroll
+        for (int i = 0; i < kHeld; i += kList) sort_falling<kList>(c + i);
+#pragma unroll
+        for (int i = 0; i < kHeld; ++i) held[i] = b ? __builtin_fmax(held[i], c[kHeld - 1 - i]) : c[i];
+        if (kPer > kHeld && b) merge_falling<kHeld>(held);
+    }
+    double chosen = 0.0;
     for (int j = 0; j < k; ++j) {
-        unsigned best = key[0];
+        double best = held[0];
 #pragma unroll
-        for (int i = 1; i < kPer; ++i) best = max(best, key[i]);
-        const unsigned top = row_max_u32(best);
-        unsigned at = 0x7fffffffu;
+        for (int i = kList; i < kHeld; i += kList) best = __builtin_fmax(best, held[i]);
+        const double top = row_max(best);
 #pragma unroll
-        for (int i = kPer - 1; i >= 0; --i) at = key[i] == top ? (unsigned)(r * kPer + i) : at;
-        const unsigned e = row_min_u32(at);
+        for (int h = 0; h < kHeld; h += kList) {
+            const bool taken = __double2loint(held[h]) == __double2loint(top);  // the index is in the low word
 #pragma unroll
-        for (int i = 0; i < kPer; ++i) key[i] = e == (unsigned)(r * kPer + i) ? 0u : key[i];
-        if (r == j) chosen = top, expert = (int)e;
+            for (int i = 0; i < kList; ++i) {
+                const double here = held[h + i], next = i + 1 < kList ? held[h + i + 1] : 0.0;
+                held[h + i] = taken ? next : here;
+            }
+        }
+        if (r == j) chosen = top;
     }
     // softmax over the chosen: against the largest, infinities taken as the largest finite number, nothing for -inf
-    const float l = logit_of_key(chosen);
+    expert = index_of(chosen);
+    const float l = logit_of(chosen);
     const float finite = __builtin_fminf(__builtin_fmaxf(l, -FLT_MAX), FLT_MAX);
     const float p = r < k && l != -__builtin_inff() ? expf(finite - __shfl(finite, row)) : 0.0f;
-    float sum = 0.0f;
-    for (int j = 0; j < k; ++j) sum += __shfl(p, row + j);
+    const float sum = row_sum(p);
     gate = sum > 0.0f ? __fdiv_rn(p, sum) : 0.0f;
 }
 
@@ -82,15 +142,12 @@ template <int kPer>
 __device__ __forceinline__ void choose_run(const float* __restrict__ logits, int64_t t0, int64_t t1, int n_experts, int k, int32_t* __restrict__ experts,
                                            float* __restrict__ gates, int* hist, int* here)
 {
-    constexpr int kTokens = kRouteThreads / 16;
+    const int tokens = (int)blockDim.x / 16;
     const int r = threadIdx.x & 15;
-    for (int64_t t = t0 + threadIdx.x / 16; t - threadIdx.x / 16 < t1; t += kTokens) {  // every lane stays to the end: the reductions are a row's
-        float raw[kPer];
-#pragma unroll
-        for (int i = 0; i < kPer; ++i) raw[i] = t < t1 && r * kPer + i < n_experts ? logits[t * n_experts + r * kPer + i] : 0.0f;
+    for (int64_t t = t0 + threadIdx.x / 16; t - (threadIdx.x & 63) / 16 < t1; t += tokens) {  // a wave's lanes stay together: the reductions are a row's
         int e;
         float g;
-        choose<kPer>(raw, n_experts, k, e, g);
+        choose<kPer>(logits + min(t, t1 - 1) * n_experts, n_experts, k, e, g);
         if (t < t1 && r < k) {
             experts[t * k + r] = e;
             gates[t * k + r] = g;
@@ -183,12 +240,12 @@ template <int kPer>
 __global__ __launch_bounds__(kRouteThreads) void route_choose_kernel(RouteArgs a)
 {
     __shared__ int hist[kRouteExperts];
-    for (int e = threadIdx.x; e < a.n_experts; e += kRouteThreads) hist[e] = 0;
+    for (int e = threadIdx.x; e < a.n_experts; e += (int)blockDim.x) hist[e] = 0;
     __syncthreads();
     const int64_t t0 = blockIdx.x * a.run, t1 = min(t0 + a.run, a.T);
     choose_run<kPer>(a.logits, t0, t1, a.n_experts, a.k, a.experts, a.gates, hist, nullptr);
     __syncthreads();
-    for (int e = threadIdx.x; e < a.n_experts; e += kRouteThreads) a.work[blockIdx.x * a.n_experts + e] = hist[e];
+    for (int e = threadIdx.x; e < a.n_experts; e += (int)blockDim.x) a.work[blockIdx.x * a.n_experts + e] = hist[e];
 }
 
 __global__ __launch_bounds__(kRouteThreads) void route_place_kernel(RouteArgs a)
@@ -226,7 +283,7 @@ __global__ __launch_bounds__(kRouteThreads) void route_place_kernel(RouteArgs a)
 template <int kPer>
 __global__ __launch_bounds__(kRouteThreads) void route_single_kernel(RouteArgs a)
 {
-    __shared__ int hist[kRouteExperts], base[kRouteExperts], scratch[kRouteWaves], here[kRouteLeast * Q8_ROUTE_MAX_K];
+    __shared__ int hist[kRouteExperts], base[kRouteExperts], scratch[kRouteWaves], here[kRouteSinglePairs];
     __shared__ int count[kRouteWaves * kRouteExperts];
     const Part q = part_of_wave(0, a.T * a.k);
     for (int e = threadIdx.x; e < a.n_experts; e += kRouteThreads) hist[e] = base[e] = 0;
@@ -243,11 +300,19 @@ __global__ __launch_bounds__(kRouteThreads) void route_single_kernel(RouteArgs a
 template <int kPer>
 static int launch(RouteArgs a, hipStream_t st)
 {
-    if (a.runs == 1) {
+    // One launch of one workgroup while it has little to search (one launch and two: 128 tokens, 2 of 64 experts 5.9 and 7.1 us; 32 tokens, 8 of 256 7.0 and 8.3, 64
+    // tokens 9.6 and 8.6; 128 tokens, 8 of 64 8.8 and 7.2).  Else short runs, of many units, and shorter ones where a token takes long (1024 tokens, 8 of 256 experts,
+    // runs of 16 tokens 10.0 us, of 32 10.6, of 64 13.6; 512 tokens, 2 of 64 7.3, 7.2 and 7.0).
+    if (a.T <= 128 && a.T * a.k <= kRouteSinglePairs && a.T * kPer * (a.k > 4 ? a.k : 4) <= 4096) {
+        a.run = a.T;
         hipLaunchKernelGGL(route_single_kernel<kPer>, dim3(1), dim3(kRouteThreads), 0, st, a);
         return hipGetLastError() == hipSuccess ? 0 : 1;
     }
-    hipLaunchKernelGGL(route_choose_kernel<kPer>, dim3((unsigned)a.runs), dim3(kRouteThreads), 0, st, a);
+    const int64_t least = kPer < 16 ? 32 : 16, most = (a.T + kRouteBlocks - 1) / kRouteBlocks;
+    a.run = most > least ? most : least;
+    a.runs = (int)((a.T + a.run - 1) / a.run);
+    const int threads = (int)(a.run * 16 < kRouteThreads ? (a.run * 16 + 63) / 64 * 64 : kRouteThreads);
+    hipLaunchKernelGGL(route_choose_kernel<kPer>, dim3((unsigned)a.runs), dim3((unsigned)threads), 0, st, a);
     if (hipGetLastError() != hipSuccess) return 1;
     hipLaunchKernelGGL(route_place_kernel, dim3((unsigned)a.runs), dim3(kRouteThreads), 0, st, a);
     return hipGetLastError() == hipSuccess ? 0 : 1;
@@ -256,8 +321,7 @@ static int launch(RouteArgs a, hipStream_t st)
 int launch_route(const float* logits, int64_t T, int n_experts, int k, int32_t* experts, float* gates, int32_t* group_rows, int32_t* rows, int32_t* slots,
                  int32_t* work, hipStream_t st)
 {
-    const int64_t most = (T + kRouteBlocks - 1) / kRouteBlocks, run = most > kRouteLeast ? most : kRouteLeast;
-    const RouteArgs a{logits, T, run, n_experts, k, T ? (int)((T + run - 1) / run) : 1, experts, gates, group_rows, rows, slots, work};
+    const RouteArgs a{logits, T, 0, n_experts, k, 0, experts, gates, group_rows, rows, slots, work};
     if (n_experts <= 64) return launch<4>(a, st);
     if (n_experts <= 128) return launch<8>(a, st);
     if (n_experts <= 256) return launch<16>(a, st);

@@ -446,6 +446,30 @@ def test_route_masked_infinite_and_nan_logits(q8, T, E, k):
     check_route(q8, l, k)
 
 
+@pytest.mark.parametrize("E", [16, 64, 100, 128, 256, 500, 1024])
+def test_route_where_one_lane_holds_the_largest(q8, E):
+    """Equal logits; and the largest ones every sixteenth, in the last ones alone, rising and falling with the index, masked ones and NaN between."""
+    k = min(E, 16)
+    l = np.zeros((12, E), np.float32)
+    i = np.arange(E)
+    l[1, 5::16], l[2, -k:], l[3], l[4] = 1, 1, i, -i
+    l[5] = np.where(i % 16 == 3, i, -1)
+    l[6] = np.where(i % 16 == 3, -i, -np.inf)
+    l[7] = np.where(i % 3 == 0, np.nan, i // 4)
+    l[8], l[9], l[10] = -np.inf, np.nan, np.inf
+    l[11] = np.where(i < E // 2, np.float32(2.0 ** -149), np.float32(-2.0 ** -149))       # subnormal
+    check_route(q8, l, k)
+    check_route(q8, np.repeat(l, 30, 0), k)
+
+
+@pytest.mark.parametrize("T,E,k", [(31, 64, 16), (32, 64, 16), (33, 64, 16), (127, 40, 4), (128, 40, 4), (129, 40, 4), (128, 64, 5), (85, 64, 6), (86, 64, 6),
+                                   (64, 128, 8), (65, 128, 8), (32, 256, 8), (33, 256, 8), (16, 512, 4), (17, 512, 4), (8192, 64, 2), (8193, 64, 2), (4096, 160, 8), (4097, 160, 8),
+                                   (12500, 130, 2), (16385, 16, 1)])
+def test_route_where_its_launches_change(q8, T, E, k):
+    g = np.random.default_rng(T + E)
+    check_route(q8, (np.round(g.standard_normal((T, E)) * 32) / 32).astype(np.float32), k)
+
+
 def test_route_everything_to_one_expert(q8):
     l = np.zeros((1000, 16), np.float32)
     l[:, 11] = 5
