@@ -25,7 +25,10 @@ __device__ __forceinline__ void lds_dma4(v4i rsrc, unsigned voff, unsigned lds_a
 // kOut: the type of y.  It decides which operand the MFMA takes first, that is, what a lane holds of a 32x32 block.
 //   fp32, bf16    x first: one column and 16 rows.  32 lanes store 32 neighbours of a row at once, whole 128-byte lines of fp32.  (With a row and 16
 //                 columns a lane, stores take 16 bytes a lane but 32 bytes of 32 rows each, four times the requests to the L2: 12288 x 1024 -> 4096 to fp32
-//                 59 us against 48; through LDS to whole lines 56; two columns of every other row a lane, exchanged in pairs, 50 against 45.)
+//                 59 us against 48; through LDS to whole lines 56.)
+//                 bf16: of two blocks a lane has the columns 2 l and 2 l + 1, a word of y, and 32 lanes a line.  Which column a lane has is a matter of which
+//                 row of w lies in its row of LDS, so this costs nothing (24576 rows of 16 experts, 1024 -> 4096 90 us; with the columns l and 32 + l exchanged
+//                 between lanes 98).  fp32 the same way, 8 bytes a lane: on 4-bit codes no difference, on int8 42.7 against 38.5 (24576 rows, 1024 -> 1024).
 //   4-bit, int8   w first: one row and four times four neighbouring columns.  A block of the 4-bit format -- 32 neighbours of a row -- is two
 //                 lanes', its largest magnitude one exchange away.
 // The bias is what the sums start from.
@@ -36,6 +39,7 @@ __global__ __launch_bounds__(WGM* WGN * 64, kWgs* WGM* WGN / 4) void product_til
     constexpr bool kRowLane = kOut == Q8_TYPE_MX4 || kOut == Q8_TYPE_I8;
     constexpr int NW = WGM * WGN;
     constexpr int TM = BM / WGM, TN = BN / WGN, FM = TM / 32, FN = TN / 32;
+    constexpr bool kPairs = kOut == Q8_TYPE_BF16 && FN % 2 == 0;
     constexpr int A_BYTES = BM * kBK, B_BYTES = BN * kBK, OPERANDS = A_BYTES + B_BYTES;
     constexpr int SCALES = Op::kMx4 ? (BM + BN) * 8 : 0, SLOT = OPERANDS + SCALES;  // scales: [A | B][group of the stage][row]
     constexpr int A_LOADS = BM / 8 / NW, B_LOADS = BN / 8 / NW;
@@ -86,12 +90,15 @@ __global__ __launch_bounds__(WGM* WGN * 64, kWgs* WGM* WGN / 4) void product_til
 #pragma unroll
     for (int i = 0; i < B_LOADS; ++i) {
         const int g = wave * B_LOADS + i;
-        b_off[i] = (unsigned)row8 * (unsigned)pitch + (unsigned)(g * 8 * pitch) + chunk_at(g);
+        if constexpr (kPairs)  // row 2 (s % 32) + s / 32 % 2 of 64 in LDS row s = 8 g + row8
+            b_off[i] = (unsigned)(2 * row8) * (unsigned)pitch + (unsigned)((g / 8 * 64 + g % 4 * 16 + g / 4 % 2) * pitch) + chunk_at(g);
+        else
+            b_off[i] = (unsigned)row8 * (unsigned)pitch + (unsigned)(g * 8 * pitch) + chunk_at(g);
     }
     // The scale loads of this wave, 64 rows of one group of a stage each.
     const auto scale_row = [&](int i) {  // row of the operand that load i takes to this lane
         const int u = wave + i * NW;
-        return u < BM / 32 ? u % (BM / 64) * 64 + lane : (u - BM / 32) % (BN / 64) * 64 + lane;
+        return u < BM / 32 ? u % (BM / 64) * 64 + lane : (u - BM / 32) % (BN / 64) * 64 + (kPairs ? 2 * l32 + hi : lane);
     };
     if (p.x_rows) {
         int id[A_LOADS], scale_id[S_LOADS ? S_LOADS : 1];  // all asked for before the first is looked at
@@ -161,6 +168,7 @@ __global__ __launch_bounds__(WGM* WGN * 64, kWgs* WGM* WGN / 4) void product_til
     };
 
     const int wm = wave / WGN, wn = wave % WGN;
+    const auto column = [&](int j) { return kPairs ? j / 2 * 64 + 2 * l32 + j % 2 : j * 32 + l32; };  // of the wave's, this lane's of block j if it has one
     // Where this lane finds its 16 bytes of step ks in the first block of its wave's rows.  32 rows on, a row's swizzle differs in bit 2 alone,
     // so the block behind is 4 KiB away and the chunk's bit flipped: the blocks need no addresses of their own.
     static_assert((TM == 32 || TM % 64 == 0) && (TN == 32 || TN % 64 == 0), "the swizzles of a wave's blocks");
@@ -200,7 +208,7 @@ __global__ __launch_bounds__(WGM* WGN * 64, kWgs* WGM* WGN / 4) void product_til
                     for (int e = 0; e < 4; ++e) acc[i][j][4 * q + e] = c[e];
             }
         } else {
-            const Sum c = first[wn * TN + j * 32 + l32];
+            const Sum c = first[wn * TN + column(j)];
 #pragma unroll
             for (int i = 0; i < FM; ++i)
 #pragma unroll
@@ -295,7 +303,7 @@ __global__ __launch_bounds__(WGM* WGN * 64, kWgs* WGM* WGN / 4) void product_til
             if (p.flags & Q8_EPI_ABSMAX) {
 #pragma unroll
                 for (int e = 0; e < 16; ++e) {
-                    const int along = 8 * (e >> 2) + 4 * hi + (e & 3), m = wm * TM + i * 32 + (kRowLane ? l32 : along), n = n0 + wn * TN + j * 32 + (kRowLane ? along : l32);
+                    const int along = 8 * (e >> 2) + 4 * hi + (e & 3), m = wm * TM + i * 32 + (kRowLane ? l32 : along), n = n0 + wn * TN + (kRowLane ? j * 32 + along : column(j));
                     if (m < tile.rows && n < N) famax = __builtin_fmaxf(famax, __builtin_fabsf(v[e]));
                 }
             }
@@ -375,12 +383,9 @@ __global__ __launch_bounds__(WGM* WGN * 64, kWgs* WGM* WGN / 4) void product_til
         }
     } else {
         // Rows of a block lie in registers, so a row's place is a scalar offset -- which the bounds check does not see: tiles that are cut short add it to
-        // the lane's own.  bf16, if rows are whole words: two blocks beside each other have 64 columns, a line of a row.  The even lanes store two neighbours of the
-        // first, the odd ones of the second, for one row and then for the next (a block by itself would store half lines of two rows at once: 24576 rows of 16
-        // experts, 1024 -> 4096 85.6 us against 82.7, 12288 rows without groups 42.2 against 41).
-        const bool odd = lane & 1, words = kOut == Q8_TYPE_BF16 && FN % 2 == 0 && row_bytes % 4 == 0 && reinterpret_cast<uintptr_t>(p.y) % 4 == 0;
-        // v_perm_b32(mine, other): the low halves, the lower lane's first, and the high halves
-        const unsigned low = odd ? 0x05040100u : 0x01000504u, high = odd ? 0x07060302u : 0x03020706u;
+        // the lane's own.
+        constexpr int kStep = kPairs ? 2 : 1;
+        const bool words = kPairs && N % 2 == 0 && reinterpret_cast<uintptr_t>(p.y) % 4 == 0;
         auto store_tile = [&](auto fullc, auto streamc) {
             constexpr bool kFull = decltype(fullc)::value;
             constexpr int kAux = decltype(streamc)::value ? 2 : 0;  // aux bit 1: non-temporal
@@ -393,39 +398,30 @@ __global__ __launch_bounds__(WGM* WGN * 64, kWgs* WGM* WGN / 4) void product_til
                     __builtin_amdgcn_raw_buffer_store_b16(value, ry, to, uniform, kAux);
             };
 #pragma unroll
-            for (int j = 0; j < FN; ++j) {
-                const int n = n0 + wn * TN + j * 32 + l32;
-                const unsigned at = n < N ? (unsigned)(4 * hi * row_bytes + n * kSize) : kOutOfRange;
+            for (int j = 0; j < FN; j += kStep) {
+                const int n = n0 + wn * TN + column(j);
+                const unsigned at = n < N ? (unsigned)(4 * hi * row_bytes + n * kSize) : kOutOfRange, beside = n + 1 < N ? at + kSize : kOutOfRange;
 #pragma unroll
                 for (int i = 0; i < FM; ++i) {
                     const int m = wm * TM + i * 32;
-                    if (words) {
-                        if constexpr (kOut == Q8_TYPE_BF16 && FN % 2 == 0) {
-                            if (j % 2) continue;
-                            float v[16], w[16];
-                            block_values(i, j, v);
-                            block_values(i, j + 1, w);
-                            const int pair = n0 + wn * TN + j * 32 + (odd ? 32 + l32 - 1 : l32);
-                            const unsigned pair_at = pair < N ? (unsigned)(4 * hi * row_bytes + pair * 2) : kOutOfRange;
+                    float v[kStep][16];
 #pragma unroll
-                            for (int e = 0; e < 16; e += 2) {
-                                const unsigned a = f32_to_bf16x2(v[e], v[e + 1]), b = f32_to_bf16x2(w[e], w[e + 1]);
-                                const unsigned mine = odd ? b : a;
-                                const unsigned other = (unsigned)__builtin_amdgcn_update_dpp(0, (int)(odd ? a : b), 0xB1, 0xf, 0xf, true);  // quad_perm [1, 0, 3, 2]
-                                store(__builtin_amdgcn_perm(mine, other, low), pair_at, m + 8 * (e >> 2) + (e & 3));
-                                store(__builtin_amdgcn_perm(mine, other, high), pair_at, m + 8 * (e >> 2) + (e & 3) + 1);
-                            }
+                    for (int h = 0; h < kStep; ++h) block_values(i, j + h, v[h]);
+                    if (words) {
+                        if constexpr (kPairs) {
+#pragma unroll
+                            for (int e = 0; e < 16; ++e) store(f32_to_bf16x2(v[0][e], v[1][e]), at, m + 8 * (e >> 2) + (e & 3));
                         }
                     } else {
-                        float v[16];
-                        block_values(i, j, v);
 #pragma unroll
-                        for (int e = 0; e < 16; ++e) {
-                            if constexpr (kOut == Q8_TYPE_F32)
-                                store(__float_as_uint(v[e]), at, m + 8 * (e >> 2) + (e & 3));
-                            else
-                                store(f32_to_bf16(v[e]), at, m + 8 * (e >> 2) + (e & 3));
-                        }
+                        for (int h = 0; h < kStep; ++h)
+#pragma unroll
+                            for (int e = 0; e < 16; ++e) {
+                                if constexpr (kOut == Q8_TYPE_F32)
+                                    store(__float_as_uint(v[h][e]), h ? beside : at, m + 8 * (e >> 2) + (e & 3));
+                                else
+                                    store(f32_to_bf16(v[h][e]), h ? beside : at, m + 8 * (e >> 2) + (e & 3));
+                            }
                     }
                 }
             }

@@ -179,6 +179,25 @@ def test_linear(q8, variant, M, K, N, kind, gelu):
     check_product(no_bias, ref, mag, K, gelu, kind)
 
 
+@pytest.mark.parametrize("N", [1, 127, 130, 192, 449, 512])
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+def test_linear_outputs_at_any_element(q8, variant, N, kind):
+    """The same numbers wherever y starts, in full tiles and in cut ones, and nothing around them written."""
+    g = np.random.default_rng(N)
+    M, K = 517, 288
+    xq, wq, b = quantized(q8, dev(tensor(g, M, K, spread=0.5))), quantized(q8, dev(tensor(g, N, K, spread=0.5))), dev(tensor(g, 1, N, spread=0.5)).view(-1)
+    first = None
+    for offset in (0, 1, 2, 3):
+        room = torch.full((offset + M * N + 200,), 7, dtype=TYPES[kind], device="cuda")
+        y = room[offset: offset + M * N].view(M, N)
+        q8.q8_mx4_linear(*xq, *wq, b, y)
+        first = y.clone() if first is None else first
+        assert torch.equal(y, first)
+        assert (room[:offset] == 7).all() and (room[offset + M * N:] == 7).all()
+    xv, wv = (MX.values(host(c), host(s), K) for c, s in (xq, wq))
+    check_product(first, *MX.grouped(xv, [wv], [host(b)], [M], M), K, False, kind)
+
+
 @pytest.mark.parametrize("M,K,N", [(1, 1024, 4096), (7, 100, 128), (33, 768, 256), (300, 1000, 384), (1024, 512, 1024), (2500, 256, 2048)])
 @pytest.mark.parametrize("gelu", [False, True])
 def test_linear_to_codes(q8, variant, M, K, N, gelu):
