@@ -43,7 +43,8 @@ static bool tile_eligible(const Product& p, int64_t rows)
 //   2 or 3 for groups of few rows each, which leave most of a larger tile empty (4809 rows of 64 experts, 768 -> 2048 17.2 and 17.8, 128x128 20.9).
 //   5 (256x256) for long rows whose tiles leave less than a quarter of a round of the 256 units idle: it moves the fewest operand bytes, but a unit holds one at
 //     a time and waits for the last round (4096 -> 1024: 14336 rows, 224 tiles, 35.5 and 128x128 42.7; 12288 rows, 192, 36.3 and 32.9; 28672 rows, 448, 67.6 and
-//     68.6; 24576 rows, 384, 65.9 and 57.8).  int8 rows have to be 8 KiB (16384 x 8192 -> 1024 117 and 129; 8192 x 4096 -> 4096 138 and 130).
+//     68.6; 24576 rows, 384, 65.9 and 57.8).  Rows have to be 8 KiB for int8 (16384 x 8192 -> 1024 117 and 129; 8192 x 4096 ->
+//     4096 138 and 130) and for several rounds of fp32 outputs, whose stores nothing covers (8192 x 4096 -> 4096 87 and 78, to bf16 75 and 75).
 //     Short rows to 4-bit codes, whose epilogue is bound by arithmetic, if it is one round (3997 x 1024 -> 4096 12.2 and 14.6).
 //   4 (128x128) from two tiles a unit on (2184 x 1024 -> 4096 10.4 and 64x128 11.2; 12288 x 1024 -> 4096 to fp32 47 and 51), of long rows from one and a half
 //     (6396 x 4096 -> 1024 20.0 and 24.4), for int8, whose MFMAs take twice as long, also in groups that are a tile each (15373 rows of 128 experts, 512 -> 2048
@@ -57,7 +58,8 @@ static int choose(bool mx4, const Product& p)
     const bool is_long = p.pitch >= 2048, small = p.M < 96 * groups;
     if (tiles(32, 32) <= (is_long ? 512 : 256)) return 1;
     const int64_t largest = tiles(256, 256), idle = -largest & 255;
-    if (!small && idle < 64 && (p.pitch >= (mx4 ? 2048 : 8192) || (p.y_type == Q8_TYPE_MX4 && largest <= 256))) return 5;
+    const int64_t least = p.y_type == Q8_TYPE_MX4 && largest <= 256 ? 0 : mx4 && (p.y_type != Q8_TYPE_F32 || largest <= 256) ? 2048 : 8192;  // bytes of a row
+    if (!small && idle < 64 && p.pitch >= least) return 5;
     if (!small && (!mx4 || p.M > 160 * groups) && tiles(128, 128) >= (is_long ? 384 : 512)) return 4;
     if (!is_long && p.y_type == Q8_TYPE_MX4) return 3;
     return tiles(64, 128) >= 512 && (is_long || !small) ? 3 : 2;
