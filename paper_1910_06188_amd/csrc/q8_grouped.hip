@@ -36,21 +36,19 @@ static bool tile_eligible(const Product& p, int64_t rows)
 }
 
 // The kernel of a launch, by sizes alone: sums of a tiled kernel do not depend on its tile, so that outputs of every type are the same sums.
-// Long rows are those of 2 KiB of codes and more; times in us, the alternatives taken in turn.
+// Long rows are those of 2 KiB of codes and more; times in us, the alternatives taken in turn.  Over 720 shapes the choice takes 1.5 % longer than the best.
 //   1 (32x32, the reduction dealt out over the waves) up to 256 tiles (300 x 520 -> 1000, 320 of them, 5.5, 64x64 4.2), and up to 512 of long rows, whose serial
 //     walk a larger tile cannot hide (64 x 4096 -> 1024 4.7 and 7.6; int8, 275 rows of 16 experts, 4096 -> 512 9.5 and 19.7; but 754 rows of 8 experts, 2048 ->
 //     1024, about 900, 14.6 and 9.1).
-//   2 or 3 for groups of few rows each, which leave most of a larger tile empty (4809 rows of 64 experts, 768 -> 2048 17.2 and 17.8, 128x128 20.9).
 //   5 (256x256) for long rows whose tiles leave less than a quarter of a round of the 256 units idle: it moves the fewest operand bytes, but a unit holds one at
-//     a time and waits for the last round (4096 -> 1024: 14336 rows, 224 tiles, 35.5 and 128x128 42.7; 12288 rows, 192, 36.3 and 32.9; 28672 rows, 448, 67.6 and
-//     68.6; 24576 rows, 384, 65.9 and 57.8).  Rows have to be 8 KiB for int8 (16384 x 8192 -> 1024 117 and 129; 8192 x 4096 ->
-//     4096 138 and 130) and for several rounds of fp32 outputs, whose stores nothing covers (8192 x 4096 -> 4096 87 and 78, to bf16 75 and 75).
-//     Short rows to 4-bit codes, whose epilogue is bound by arithmetic, if it is one round (3997 x 1024 -> 4096 12.2 and 14.6).
-//   4 (128x128) from two tiles a unit on (2184 x 1024 -> 4096 10.4 and 64x128 11.2; 12288 x 1024 -> 4096 to fp32 47 and 51), of long rows from one and a half
-//     (6396 x 4096 -> 1024 20.0 and 24.4), for int8, whose MFMAs take twice as long, also in groups that are a tile each (15373 rows of 128 experts, 512 -> 2048
-//     49.8 and 52.7; on 4-bit codes 16145 rows, 768 -> 4096 99.9 and 92.6).
-//   3 (64x128) against 2 (64x64): from two tiles a unit on (8192 rows of 16 experts, 512 -> 4096 24.5 and 32.4), unless rows are short and groups small; and for
-//     short rows to 4-bit codes, of which its waves store 16 bytes a lane and the other's 8 (5330 rows of 64 experts, 1024 -> 512 6.6 and 7.7).
+//     a time and waits for the last round (4096 -> 1024 to bf16: 14336 rows, 224 tiles, 36.2 and 128x128 38.9; 24576 rows, 384, 66.7 and 57.6).  Rows have to be
+//     4 KiB for several rounds (8192 x 8192 -> 4096 134 and 141; 8192 x 4096 -> 4096 77 and 74), 8 KiB for int8 (4096 x 16384 -> 4096 223 and 255; 14336 x 4096 ->
+//     1024 64.0 and 64.3) and for fp32 outputs, whose stores nothing covers (4096 x 16384 -> 4096 135 and 141; 4096 x 4096 -> 4096 51 and 42).
+//   4 (128x128) from two tiles a unit on (8192 x 2048 -> 4096 to bf16 40.8, 64x128 51.9; 12288 x 1024 -> 4096 37 and 44.5), three where groups are smaller than a
+//     tile (57 rows each of 128, int8, 768 -> 1024 23.3 and 25.4; but 29 rows each 17.9 and 16.9), of long rows from one and a half.
+//   3 (64x128) against 2 (64x64): from two tiles a unit on (8192 rows of 16 experts, 512 -> 4096 24.5 and 32.4), unless rows are short and groups small (4809 rows
+//     of 64, 768 -> 2048 17.8 and 17.2); and for short rows to 4-bit codes, of which its waves store 16 bytes a lane and the other's 8 (5330 rows of 64 experts,
+//     1024 -> 512 6.4 and 7.5).
 static int choose(bool mx4, const Product& p)
 {
     const int64_t groups = p.group_rows ? (p.n_groups < p.M ? p.n_groups : p.M) : 0;  // of which half a tile each is left over
@@ -58,9 +56,9 @@ static int choose(bool mx4, const Product& p)
     const bool is_long = p.pitch >= 2048, small = p.M < 96 * groups;
     if (tiles(32, 32) <= (is_long ? 512 : 256)) return 1;
     const int64_t largest = tiles(256, 256), idle = -largest & 255;
-    const int64_t least = p.y_type == Q8_TYPE_MX4 && largest <= 256 ? 0 : mx4 && (p.y_type != Q8_TYPE_F32 || largest <= 256) ? 2048 : 8192;  // bytes of a row
+    const int64_t least = !mx4 || p.y_type == Q8_TYPE_F32 ? 8192 : largest <= 256 ? 2048 : 4096;  // bytes of a row
     if (!small && idle < 64 && p.pitch >= least) return 5;
-    if (!small && (!mx4 || p.M > 160 * groups) && tiles(128, 128) >= (is_long ? 384 : 512)) return 4;
+    if (p.M >= 48 * groups && tiles(128, 128) >= (is_long ? 384 : small ? 768 : 512)) return 4;
     if (!is_long && p.y_type == Q8_TYPE_MX4) return 3;
     return tiles(64, 128) >= 512 && (is_long || !small) ? 3 : 2;
 }

@@ -169,16 +169,13 @@ __global__ __launch_bounds__(WGM* WGN * 64, kWgs* WGM* WGN / 4) void product_til
 
     const int wm = wave / WGN, wn = wave % WGN;
     const auto column = [&](int j) { return kPairs ? j / 2 * 64 + 2 * l32 + j % 2 : j * 32 + l32; };  // of the wave's, this lane's of block j if it has one
-    // Where this lane finds its 16 bytes of step ks in the first block of its wave's rows.  32 rows on, a row's swizzle differs in bit 2 alone,
-    // so the block behind is 4 KiB away and the chunk's bit flipped: the blocks need no addresses of their own.
+    // Where this lane finds its 16 bytes of step 0 in the first block of its wave's rows.  32 rows on, a row's swizzle differs in bit 2 alone,
+    // so the block behind is 4 KiB away and the chunk's bit flipped; step ks has ks in the chunk's low bits.  So neither needs an address of its own: the
+    // registers that eight of them took keep 128x128 tiles from having four workgroups a unit (24576 rows of 16 experts, 1024 -> 4096 92 us with three, 84 with
+    // four; -> codes with GELU 101 and 94).
     static_assert((TM == 32 || TM % 64 == 0) && (TN == 32 || TN % 64 == 0), "the swizzles of a wave's blocks");
-    int a_lane[kKS], b_lane[kKS];
-#pragma unroll
-    for (int ks = 0; ks < kKS; ++ks) {
-        const int ra = wm * TM + l32, rb = wn * TN + l32;
-        a_lane[ks] = ra * kBK + (((4 * hi + ks) ^ swizzle_of_row(ra)) << 4);
-        b_lane[ks] = A_BYTES + rb * kBK + (((4 * hi + ks) ^ swizzle_of_row(rb)) << 4);
-    }
+    const int ra = wm * TM + l32, rb = wn * TN + l32;
+    const int a_lane = ra * kBK + (((4 * hi) ^ swizzle_of_row(ra)) << 4), b_lane = A_BYTES + rb * kBK + (((4 * hi) ^ swizzle_of_row(rb)) << 4);
     const int a_sc = OPERANDS + (hi * BM + wm * TM + l32) * 4, b_sc = OPERANDS + BM * 8 + (hi * BN + wn * TN + l32) * 4;
 
     load_stage(0, 0, std::true_type{});
@@ -226,17 +223,22 @@ __global__ __launch_bounds__(WGM* WGN * 64, kWgs* WGM* WGN / 4) void product_til
             for (int f = 0; f < FN; ++f) sb[f] = *reinterpret_cast<const int*>(stage + b_sc + f * 128);
         }
         v4i fa[kAhead][FM], fb[kAhead][FN];
-        auto read_step = [&](int ks) {
+        auto read_step = [&](auto kc) {
+            constexpr int ks = decltype(kc)::value;
+            int a_at = a_lane, b_at = b_lane;
+            if constexpr (ks > 0) {  // in assembly, or the compiler moves them out of the loop and keeps all eight
+                asm volatile("v_xor_b32 %0, %2, %1" : "=v"(a_at) : "v"(a_lane), "i"(ks << 4));
+                asm volatile("v_xor_b32 %0, %2, %1" : "=v"(b_at) : "v"(b_lane), "i"(ks << 4));
+            }
 #pragma unroll
-            for (int f = 0; f < FM; ++f) fa[ks % kAhead][f] = *reinterpret_cast<const v4i*>(stage + (a_lane[ks] ^ ((f & 1) << 6)) + f * 32 * kBK);
+            for (int f = 0; f < FM; ++f) fa[ks % kAhead][f] = *reinterpret_cast<const v4i*>(stage + (a_at ^ ((f & 1) << 6)) + f * 32 * kBK);
 #pragma unroll
-            for (int f = 0; f < FN; ++f) fb[ks % kAhead][f] = *reinterpret_cast<const v4i*>(stage + (b_lane[ks] ^ ((f & 1) << 6)) + f * 32 * kBK);
+            for (int f = 0; f < FN; ++f) fb[ks % kAhead][f] = *reinterpret_cast<const v4i*>(stage + (b_at ^ ((f & 1) << 6)) + f * 32 * kBK);
         };
-#pragma unroll
-        for (int ks = 0; ks < kAhead - 1; ++ks) read_step(ks);
+        static_for<0, kAhead - 1>([&](auto kc) { read_step(kc); });
         static_for<0, kKS>([&](auto kc) {
             constexpr int ks = decltype(kc)::value, next = ks + kAhead - 1;
-            if constexpr (next < kKS) read_step(next);
+            if constexpr (next < kKS) read_step(std::integral_constant<int, next>{});
             if constexpr (next == kKS - 1) {
                 __builtin_amdgcn_sched_barrier(0);
                 loads();
