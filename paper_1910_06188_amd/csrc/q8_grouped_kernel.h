@@ -3,7 +3,8 @@
 // A workgroup owns BM rows of one group and BN columns of the group's weights.  It walks the reduction in stages of 128 bytes a row
 // (128 int8 codes, 256 4-bit ones), loaded straight into LDS by 16 bytes a lane, swizzled so that the fragment reads of the MFMAs
 // are free of bank conflicts.  The scales of a stage (4-bit: two words a row) come into LDS with it, four bytes a lane.  kSlots stage
-// buffers: one (load, wait, multiply; other workgroups of the unit fill the gaps) or two (the next stage loads under this one's MFMAs).
+// buffers: one (load, wait, multiply; other workgroups of the unit fill the gaps) or two (the next stage loads under this one's MFMAs).  128x128
+// tiles have one: two buffers and half the workgroups are 10 to 20 % slower.  256x256 have two, as a unit holds one of them.
 //
 // Loads and stores go through buffer descriptors whose bounds checks take the place of branches: a lane whose row of x does not exist, or whose
 // 16 bytes lie behind the end of a row, is given an offset out of range and reads zeros; outputs outside the tile's rows and columns are dropped.
