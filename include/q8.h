@@ -404,7 +404,7 @@ q8_status q8_mx4_quantize(const void* x, int x_type, int64_t M, int64_t K, uint8
 q8_status q8_mx4_fake_quantize(const void* x, int type, int64_t M, int64_t K, void* xq, void* stream);
 
 /*
- * The FC layer on 4-bit codes: y[m,n] = act(sum_k x[m,k] w[n,k] + bias[n]), products exact, sums in fp32.
+ * The FC layer on 4-bit codes: y[m,n] = act(sum_k x[m,k] w[n,k] + bias[n]), products exact, sums in fp32, the bias added once behind them.
  *   xq, xs: codes and scales of x [M,K]; wq, ws: of w [N,K]; bias fp32[N] or NULL.
  *   y_type Q8_TYPE_F32 or Q8_TYPE_BF16 (rounded once to nearest even): y [M,N], y_scales ignored.
  *   y_type Q8_TYPE_MX4: N a multiple of 128; y and y_scales receive the codes and scales of the fp32 result, the same bytes that

@@ -32,7 +32,8 @@ __device__ __forceinline__ void lds_dma4(v4i rsrc, unsigned voff, unsigned lds_a
 //                 between lanes 98).  fp32 the same way, 8 bytes a lane: on 4-bit codes no difference, on int8 42.7 against 38.5 (24576 rows, 1024 -> 1024).
 //   4-bit, int8   w first: one row and four times four neighbouring columns.  A block of the 4-bit format -- 32 neighbours of a row -- is two
 //                 lanes', its largest magnitude one exchange away.
-// The bias is what the sums start from.
+// The bias of int8 codes is what the sums start from, which whole numbers allow.  That of 4-bit codes is added once behind the sum: a sum that starts from it
+// would be rounded at its magnitude by every matrix instruction, K / 64 of them.
 template <class Op, int BM, int BN, int WGM, int WGN, int kSlots, int kAhead, int kWgs, int kOut>
 __global__ __launch_bounds__(WGM* WGN * 64, kWgs* WGM* WGN / 4) void product_tile_kernel(Product p, unsigned tiles_n, unsigned panel_reciprocal, int stream_out)
 {
@@ -51,7 +52,7 @@ __global__ __launch_bounds__(WGM* WGN * 64, kWgs* WGM* WGN / 4) void product_til
     static_assert(kWgs * (kSlots * SLOT + BN * 4) <= 160 * 1024, "LDS is 160 KiB per compute unit");
     using Sum = typename Op::Sum;
     __shared__ __attribute__((aligned(1024))) char lds[kSlots * SLOT];
-    __shared__ __attribute__((aligned(16))) Sum first[BN];  // what the sums of each column start from
+    __shared__ __attribute__((aligned(16))) Sum bias[BN];  // of each column, int8 the quantized one
 
     const int lane = threadIdx.x & 63, l32 = lane & 31, hi = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -185,9 +186,9 @@ __global__ __launch_bounds__(WGM* WGN * 64, kWgs* WGM* WGN / 4) void product_til
     for (int t = threadIdx.x; t < BN; t += NW * 64) {
         const ProductColumn c = product_column<Op>(p, tile.group, min(n0 + t, N - 1), sx);
         if constexpr (Op::kMx4)
-            first[t] = c.b;
+            bias[t] = c.b;
         else
-            first[t] = c.bq;
+            bias[t] = c.bq;
     }
     __builtin_amdgcn_s_waitcnt(waitcnt_vm_lgkm0(0));
     __syncthreads();
@@ -197,17 +198,17 @@ __global__ __launch_bounds__(WGM* WGN * 64, kWgs* WGM* WGN / 4) void product_til
     typename Op::Acc acc[FM][FN];
 #pragma unroll
     for (int j = 0; j < FN; ++j) {
-        if constexpr (kRowLane) {
+        if constexpr (kRowLane && !Op::kMx4) {
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
-                const v4s c = *reinterpret_cast<const v4s*>(first + wn * TN + j * 32 + 8 * q + 4 * hi);
+                const v4s c = *reinterpret_cast<const v4s*>(bias + wn * TN + j * 32 + 8 * q + 4 * hi);
 #pragma unroll
                 for (int i = 0; i < FM; ++i)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) acc[i][j][4 * q + e] = c[e];
             }
         } else {
-            const Sum c = first[wn * TN + column(j)];
+            const Sum c = Op::kMx4 ? 0 : bias[wn * TN + column(j)];
 #pragma unroll
             for (int i = 0; i < FM; ++i)
 #pragma unroll
@@ -292,12 +293,20 @@ __global__ __launch_bounds__(WGM* WGN * 64, kWgs* WGM* WGN / 4) void product_til
     float famax = 0.0f;
     // Block (i, j) as fp32 values.
     auto block_values = [&](int i, int j, float* v) {
+        if constexpr (Op::kMx4 && kRowLane) {
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
-            if constexpr (Op::kMx4)
-                v[e] = acc[i][j][e];
-            else
-                v[e] = (float)acc[i][j][e] * r;
+            for (int q = 0; q < 4; ++q) {
+                const v4s c = *reinterpret_cast<const v4s*>(bias + wn * TN + j * 32 + 8 * q + 4 * hi);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[4 * q + e] = __fadd_rn(acc[i][j][4 * q + e], c[e]);
+            }
+        } else if constexpr (Op::kMx4) {
+            const float c = bias[wn * TN + column(j)];
+#pragma unroll
+            for (int e = 0; e < 16; ++e) v[e] = __fadd_rn(acc[i][j][e], c);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 16; ++e) v[e] = (float)acc[i][j][e] * r;
         }
         if (gelu) {
 #pragma unroll
