@@ -398,10 +398,16 @@ q8_status q8_mx4_quantize(const void* x, int x_type, int64_t M, int64_t K, uint8
 
 /*
  * The quantizer of a training step: xq[m,k] = the value that the code of x[m,k] stands for (NaN in a block with an infinity or a NaN),
- * exact in either type.  Its gradient is the straight-through estimator, q8_ste_backward.
+ * exact in either type.
  *   x, xq of one type, Q8_TYPE_F32 or Q8_TYPE_BF16; xq may be x itself.
  */
 q8_status q8_mx4_fake_quantize(const void* x, int type, int64_t M, int64_t K, void* xq, void* stream);
+
+/*
+ * Its gradient, the straight-through estimator of q8_ste_backward on gradients of either type: grad_x[i] = grad_xq[i].  grad_x may be grad_xq itself (then nothing
+ * is launched); otherwise the two must not overlap.  n >= 0.
+ */
+q8_status q8_mx4_ste_backward(const void* grad_xq, int type, int64_t n, void* grad_x, void* stream);
 
 /*
  * The FC layer on 4-bit codes: y[m,n] = act(sum_k x[m,k] w[n,k] + bias[n]), products exact, sums in fp32, the bias added once behind them.

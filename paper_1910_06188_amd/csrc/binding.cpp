@@ -209,6 +209,19 @@ struct mx4_fake_quantize {  // x, xq, stream
         return unlocked([&] { return q8_mx4_fake_quantize(xp, type, M, K, q, st); });
     }
 };
+struct mx4_ste_backward {  // grad_xq, grad_x, stream
+    static constexpr int kArgs = 3;
+    static q8_status run(PyObject* const* a, const char* where)
+    {
+        const at::Tensor &g = tensor(a[0], where), &gx = tensor(a[1], where);
+        if (gx.scalar_type() != g.scalar_type()) refuse(PyExc_TypeError, where, "the gradients are of one type");
+        if (gx.numel() != g.numel()) refuse(PyExc_ValueError, where, "sizes differ");
+        const int64_t n = g.numel();
+        const int type = float_type(g, where);
+        void *from = float_data(g, where), *to = float_data(gx, where), *st = stream_of(a[2]);
+        return unlocked([&] { return q8_mx4_ste_backward(from, type, n, to, st); });
+    }
+};
 struct mx4_linear {  // xq, xs, wq, ws, bias, y, y_scales, flags, stream
     static constexpr int kArgs = 9;
     static q8_status run(PyObject* const* a, const char* where)
@@ -340,6 +353,7 @@ struct Name;
     struct Name<NAME> { static constexpr const char* kText = "q8_" #NAME; }
 Q8_NAME(mx4_quantize);
 Q8_NAME(mx4_fake_quantize);
+Q8_NAME(mx4_ste_backward);
 Q8_NAME(mx4_linear);
 Q8_NAME(mx4_linear_dynamic);
 Q8_NAME(mx4_linear_grouped);
@@ -386,6 +400,7 @@ PyMethodDef methods[] = {Q8_ENTRY(q8_absmax),
                          Q8_ENTRY(q8_attention),
                          Q8_CHECKED_ENTRY(mx4_quantize),
                          Q8_CHECKED_ENTRY(mx4_fake_quantize),
+                         Q8_CHECKED_ENTRY(mx4_ste_backward),
                          Q8_CHECKED_ENTRY(mx4_linear),
                          Q8_CHECKED_ENTRY(mx4_linear_dynamic),
                          Q8_CHECKED_ENTRY(mx4_linear_grouped),

@@ -467,6 +467,19 @@ q8_status q8_mx4_fake_quantize(const void* x, int type, int64_t M, int64_t K, vo
     return q8::launch_mx4_fake_quantize(x, type == Q8_TYPE_BF16, M, K, xq, as_stream(stream)) ? Q8_ERR_LAUNCH : Q8_OK;
 }
 
+q8_status q8_mx4_ste_backward(const void* grad_xq, int type, int64_t n, void* grad_x, void* stream)
+{
+    if (n < 0) return Q8_ERR_SHAPE;
+    if (!float_type(type)) return Q8_ERR_FLAGS;
+    if (n == 0) return Q8_OK;
+    if (!grad_xq || !grad_x) return Q8_ERR_NULL;
+    if (misaligned(grad_xq, (unsigned)type_bytes(type)) || misaligned(grad_x, (unsigned)type_bytes(type))) return Q8_ERR_ALIGN;
+    if (grad_xq != grad_x && overlap(grad_xq, n * type_bytes(type), grad_x, n * type_bytes(type))) return Q8_ERR_OVERLAP;
+    const int bad = type == Q8_TYPE_BF16 ? q8::launch_ste_backward(static_cast<const uint16_t*>(grad_xq), n, static_cast<uint16_t*>(grad_x), as_stream(stream))
+                                         : q8::launch_ste_backward(static_cast<const float*>(grad_xq), n, static_cast<float*>(grad_x), as_stream(stream));
+    return bad ? Q8_ERR_LAUNCH : Q8_OK;
+}
+
 q8_status q8_mx4_linear(const uint8_t* xq, const uint8_t* xs, const uint8_t* wq, const uint8_t* ws, const float* bias, int64_t M, int64_t N, int64_t K,
                         void* y, int y_type, uint8_t* y_scales, uint32_t flags, void* stream)
 {

@@ -493,15 +493,15 @@ __global__ __launch_bounds__(kEwThreads) void ema_update_kernel(const float* __r
     }
 }
 
-// Eq. 5: the gradient passes unchanged.  A plain streaming copy.
-template <bool kVec, bool kNt>
-__global__ __launch_bounds__(kEwThreads) void ste_backward_kernel(const float* __restrict__ g, int64_t n,
-                                                                   float* __restrict__ gx)
+// Eq. 5: the gradient passes unchanged.  A plain streaming copy of elements T (fp32, or the bits of bf16).
+template <class T, bool kVec, bool kNt>
+__global__ __launch_bounds__(kEwThreads) void ste_backward_kernel(const T* __restrict__ g, int64_t n, T* __restrict__ gx)
 {
     if (kVec) {
+        constexpr int kElems = 16 / sizeof(T);
         const float4* gv = reinterpret_cast<const float4*>(g);
         float4* ov = reinterpret_cast<float4*>(gx);
-        const int64_t nvec = n >> 2;
+        const int64_t nvec = n / kElems;
         // trips over blocks of kEwUnroll neighbouring 4 KiB pieces, block (trip * grid + b) to workgroup b (see absmax_thread)
         const int64_t step = (int64_t)gridDim.x * (kEwUnroll * kEwThreads);
         int64_t i = (int64_t)blockIdx.x * (kEwUnroll * kEwThreads) + threadIdx.x;
@@ -520,7 +520,7 @@ __global__ __launch_bounds__(kEwThreads) void ste_backward_kernel(const float* _
         for (; i < nvec; i += step)  // the ragged last block
             for (int u = 0; u < kEwUnroll && i + u * kEwThreads < nvec; ++u) ov[i + u * kEwThreads] = gv[i + u * kEwThreads];
         if (blockIdx.x == 0) {
-            int64_t t = (nvec << 2) + threadIdx.x;
+            int64_t t = nvec * kElems + threadIdx.x;
             if (t < n) gx[t] = g[t];
         }
     } else {
@@ -939,17 +939,22 @@ int launch_ema_update(const float* amax, int n_amax, float decay, float* state, 
     return hipGetLastError() == hipSuccess ? 0 : 1;
 }
 
-int launch_ste_backward(const float* g, int64_t n, float* gx, hipStream_t st)
+template <class T>
+static int launch_copy(const T* g, int64_t n, T* gx, hipStream_t st)
 {
     if (n == 0 || g == gx) return 0;
+    const int64_t nvec = n / (16 / (int64_t)sizeof(T));
     bool vec = ((reinterpret_cast<uintptr_t>(g) & 15) == 0) && ((reinterpret_cast<uintptr_t>(gx) & 15) == 0);
-    if (vec && stream_out(n))
-        hipLaunchKernelGGL((ste_backward_kernel<true, true>), dim3(ew_grid(n >> 2)), dim3(kEwThreads), 0, st, g, n, gx);
+    if (vec && stream_out(nvec * 4))
+        hipLaunchKernelGGL((ste_backward_kernel<T, true, true>), dim3(ew_grid(nvec)), dim3(kEwThreads), 0, st, g, n, gx);
     else if (vec)
-        hipLaunchKernelGGL((ste_backward_kernel<true, false>), dim3(ew_grid(n >> 2)), dim3(kEwThreads), 0, st, g, n, gx);
+        hipLaunchKernelGGL((ste_backward_kernel<T, true, false>), dim3(ew_grid(nvec)), dim3(kEwThreads), 0, st, g, n, gx);
     else
-        hipLaunchKernelGGL((ste_backward_kernel<false, false>), dim3(ew_grid(n)), dim3(kEwThreads), 0, st, g, n, gx);
+        hipLaunchKernelGGL((ste_backward_kernel<T, false, false>), dim3(ew_grid(n)), dim3(kEwThreads), 0, st, g, n, gx);
     return hipGetLastError() == hipSuccess ? 0 : 1;
 }
+
+int launch_ste_backward(const float* g, int64_t n, float* gx, hipStream_t st) { return launch_copy(g, n, gx, st); }
+int launch_ste_backward(const uint16_t* g, int64_t n, uint16_t* gx, hipStream_t st) { return launch_copy(g, n, gx, st); }
 
 }  // namespace q8

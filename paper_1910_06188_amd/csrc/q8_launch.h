@@ -51,6 +51,7 @@ int launch_fake_quantize_ema(const float* x, int64_t n, float decay, float* stat
 int launch_ema_update(const float* amax, int n_amax, float decay, float* state, float* amax_out, float* scale_out,
                       hipStream_t st);
 int launch_ste_backward(const float* g, int64_t n, float* gx, hipStream_t st);
+int launch_ste_backward(const uint16_t* g, int64_t n, uint16_t* gx, hipStream_t st);  // bf16
 
 // The Int8 GEMM with its epilogue, any shape and alignment: picks the kernel and its tile (q8_gemm.hip).
 int launch_gemm(const int8_t* xq, const int8_t* wq, int64_t M, int64_t N, int64_t K, const Epilogue& ep, hipStream_t st);

@@ -72,13 +72,14 @@ _lib.q8_debug_loop_probe.restype = C.c_int
 _lib.q8_linear_f32_slots.argtypes = [_vp, _vp, _i32, _vp, _vp, _vp, _i32, _i64, _i64, _i64, _vp, _vp, _vp, _vp, _vp, _vp, _u32, _vp]
 _lib.q8_mx4_quantize.argtypes = [_vp, _i32, _i64, _i64, _vp, _vp, _vp]
 _lib.q8_mx4_fake_quantize.argtypes = [_vp, _i32, _i64, _i64, _vp, _vp]
+_lib.q8_mx4_ste_backward.argtypes = [_vp, _i32, _i64, _vp, _vp]
 _lib.q8_mx4_linear.argtypes = [_vp, _vp, _vp, _vp, _vp, _i64, _i64, _i64, _vp, _i32, _vp, _u32, _vp]
 _lib.q8_mx4_linear_dynamic.argtypes = [_vp, _i32, _vp, _vp, _vp, _i64, _i64, _i64, _vp, _vp, _vp, _i32, _vp, _u32, _vp]
 _lib.q8_mx4_linear_grouped.argtypes = [_vp, _vp, _i64, _vp, _vp, _vp, _vp, _vp, _i32, _i64, _i64, _i64, _vp, _i32, _vp, _u32, _vp]
 _lib.q8_linear_grouped.argtypes = [_vp, _i64, _vp, _vp, _vp, _vp, _vp, _vp, _i32, _i64, _i64, _i64, _vp, _vp, _vp, _u32, _vp]
 _lib.q8_route.argtypes = [_vp, _i64, _i32, _i32, _vp, _vp, _vp, _vp, _vp, _vp, _vp]
 _lib.q8_combine.argtypes = [_vp, _i64, _vp, _vp, _i64, _i32, _i64, _vp, _i32, _vp]
-for _f in ("q8_mx4_quantize", "q8_mx4_fake_quantize", "q8_mx4_linear", "q8_mx4_linear_dynamic", "q8_mx4_linear_grouped", "q8_linear_grouped",
+for _f in ("q8_mx4_quantize", "q8_mx4_fake_quantize", "q8_mx4_ste_backward", "q8_mx4_linear", "q8_mx4_linear_dynamic", "q8_mx4_linear_grouped", "q8_linear_grouped",
            "q8_route", "q8_combine"):
     getattr(_lib, _f).restype = C.c_int
 for _f in ("q8_linear_f32_slots", "q8_attention", "q8_layernorm_absmax", "q8_embedding_sum3_layernorm", "q8_fake_quantize", "q8_ema_update", "q8_fake_quantize_ema", "q8_ste_backward", "q8_absmax", "q8_scale_from_amax", "q8_quantize", "q8_quantize_amax", "q8_linear", "q8_linear_f32", "q8_embedding",
@@ -313,9 +314,12 @@ def q8_fake_quantize_ema(x, decay, state, scal_work, xq, stream=None) -> None:
 
 
 def q8_ste_backward(grad_xq, grad_x, stream=None) -> None:
-    """Eq. 5: grad_x = grad_xq."""
+    """Eq. 5: grad_x = grad_xq, both fp32 or both bf16 (the gradients of q8_mx4_fake_quantize)."""
     if grad_x.numel() != grad_xq.numel():
         raise ValueError("q8_ste_backward: sizes differ")
+    if grad_xq.dtype is not torch.float32 or grad_x.dtype is not torch.float32:
+        _ck(_binding.q8_mx4_ste_backward(grad_xq, grad_x, _stream(stream)), "q8_ste_backward")
+        return
     _ck(_binding.q8_ste_backward(grad_xq, grad_xq.numel(), grad_x, _stream(stream)), "q8_ste_backward")
 
 

@@ -66,3 +66,40 @@ def test_a_bias_larger_than_the_sum_costs_one_rounding(q8, variant, M, K):
     q8.q8_mx4_linear_grouped(*xq, torch.stack([wq[0]] * 2), torch.stack([wq[1]] * 2), torch.stack([dev(b), -dev(b)]), counts, grouped)
     want[M // 3:] = (x[M // 3:].astype(np.float64) @ w.astype(np.float64).T).astype(np.float32) - b
     np.testing.assert_array_equal(host(grouped), want)
+
+
+# ---- the gradient of the 4-bit quantizer ---------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("n", [0, 1, 5, 8, 4099, 2_000_001, 40_000_003])
+@pytest.mark.parametrize("kind", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("offset", [0, 1])
+def test_gradient_of_either_type(q8, n, kind, offset):
+    """Every bit of the gradient, NaN among them, wherever the tensors start; nothing around it is written."""
+    bits = torch.int32 if kind is torch.float32 else torch.int16
+    room = torch.randint(torch.iinfo(bits).min, torch.iinfo(bits).max, (n + offset,), dtype=bits, device="cuda")
+    out = torch.full((offset + n + 9,), 7, dtype=bits, device="cuda")
+    grad, grad_x = room[offset:].view(kind), out[offset: offset + n].view(kind)
+    q8.q8_ste_backward(grad, grad_x)
+    assert torch.equal(out[offset: offset + n], room[offset:])
+    assert (out[:offset] == 7).all() and (out[offset + n:] == 7).all()
+    kept = room.clone()
+    q8.q8_ste_backward(grad, grad)                   # in place: nothing to do
+    assert torch.equal(room, kept)
+
+
+@pytest.mark.parametrize("kind", [torch.float32, torch.bfloat16])
+def test_a_training_step_through_the_quantizer(q8, kind):
+    """loss = sum c xq with xq the codes' values: its gradient by the estimator is c, in the type of x.  Against differences of the straight line that the
+    estimator takes the codes' values for: x itself."""
+    g = np.random.default_rng(8)
+    x, c = dev(g.standard_normal((24, 96)).astype(np.float32)).to(kind), dev(g.standard_normal((24, 96)).astype(np.float32)).to(kind)
+    xq, grad_x = torch.empty_like(x), torch.zeros_like(x)
+    q8.q8_mx4_fake_quantize(x, xq)
+    want_c, want_s = MX.quantize(host(x))
+    np.testing.assert_array_equal(host(xq), MX.values(want_c, want_s, 96))
+    q8.q8_ste_backward(c, grad_x)
+    assert grad_x.dtype is kind and torch.equal(grad_x, c)
+    loss = lambda v: float((host(c) * v).sum())  # noqa: E731
+    d = np.zeros((24, 96))
+    d[3, 40], step = 1, 0.5
+    assert abs((loss(host(x) + step * d) - loss(host(x) - step * d)) / (2 * step) - host(grad_x)[3, 40]) <= 1e-9

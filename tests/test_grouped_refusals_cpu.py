@@ -1,0 +1,48 @@
+"""What the 4-bit, grouped and routing entry points refuse before anything is launched, for calls that share memory, mix types or name sizes
+beyond any tensor."""
+import os
+
+import pytest
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+LIB = os.path.join(ROOT, "paper_1910_06188_amd", "libq8.so")
+OK, NULL, SHAPE, ALIGN, FLAGS, LAUNCH, LARGE, OVERLAP = range(8)
+F32, BF16, MX4, I8 = range(4)
+
+
+@pytest.fixture(scope="module")
+def lib():
+    if not os.path.exists(LIB):
+        from paper_1910_06188_amd import build
+        build.build()
+    from paper_1910_06188_amd import q8
+    return q8.raw()
+
+
+def at(i):
+    """Addresses far apart, never dereferenced."""
+    return (i + 1) << 40
+
+
+def test_gradients_of_other_types_are_refused():
+    import torch
+    from paper_1910_06188_amd import q8
+    f, b, h = torch.zeros(8), torch.zeros(8, dtype=torch.bfloat16), torch.zeros(8, dtype=torch.float16)
+    for grad, out in ((f, b), (b, f), (h, h), (f, h), (f.double(), f.double()), (f.int(), f.int())):
+        with pytest.raises(TypeError):
+            q8.q8_ste_backward(grad, out)
+    for grad, out in ((b, b[:4]), (f, f[:4])):
+        with pytest.raises(ValueError):
+            q8.q8_ste_backward(grad, out)
+    for grad in (f, b):
+        with pytest.raises(ValueError, match="device tensors"):
+            q8.q8_ste_backward(grad, grad.clone())
+
+
+def test_gradient_of_either_type_refuses(lib):
+    f, p, q = lib.q8_mx4_ste_backward, at(0), at(1)
+    assert f(p, F32, -1, q, None) == SHAPE and f(p, MX4, 8, q, None) == FLAGS and f(p, I8, 8, q, None) == FLAGS
+    assert f(None, BF16, 8, q, None) == NULL and f(p, BF16, 8, None, None) == NULL
+    assert f(p + 2, F32, 8, q, None) == ALIGN and f(p, BF16, 8, q + 1, None) == ALIGN
+    assert f(p, BF16, 8, p + 14, None) == OVERLAP and f(p + 28, F32, 8, p, None) == OVERLAP
+    assert f(None, BF16, 0, None, None) == OK and f(p, BF16, 8, p, None) == OK          # in place: nothing to do
