@@ -566,7 +566,8 @@ q8_status q8_route(const float* logits, int64_t T, int n_experts, int k, int32_t
 
 q8_status q8_combine(const void* y, int64_t R, const int32_t* slots, const float* gates, int64_t T, int k, int64_t N, void* out, int type, void* stream)
 {
-    if (R < 0 || T < 0 || N < 0 || k < 1 || R > kMaxRows || T > kMaxRows / k || (N > 0 && R > ((int64_t)1 << 40) / N)) return Q8_ERR_SHAPE;
+    constexpr int64_t kMost = (int64_t)1 << 40;
+    if (R < 0 || T < 0 || N < 0 || k < 1 || R > kMaxRows || T > kMaxRows / k || N > kMost || (N > 0 && R > kMost / N)) return Q8_ERR_SHAPE;
     if (!float_type(type)) return Q8_ERR_FLAGS;
     if (N > 0 && T > (((int64_t)1 << 32) - 64) / ((N * type_bytes(type) + 15) / 16)) return Q8_ERR_SHAPE;  // a thread for every 16 bytes of a row
     if (T == 0 || N == 0) return Q8_OK;

@@ -46,3 +46,9 @@ def test_gradient_of_either_type_refuses(lib):
     assert f(p + 2, F32, 8, q, None) == ALIGN and f(p, BF16, 8, q + 1, None) == ALIGN
     assert f(p, BF16, 8, p + 14, None) == OVERLAP and f(p + 28, F32, 8, p, None) == OVERLAP
     assert f(None, BF16, 0, None, None) == OK and f(p, BF16, 8, p, None) == OK          # in place: nothing to do
+
+
+@pytest.mark.parametrize("N", [(1 << 40) + 1, 1 << 60, 1 << 61, 1 << 62, (1 << 63) - 1])
+def test_combine_refuses_rows_beyond_any_tensor(lib, N):
+    for T, R, t in ((4, 0, F32), (4, 0, BF16), (1, 1, F32)):
+        assert lib.q8_combine(at(0), R, at(1), at(2), T, 2, N, at(3), t, None) == SHAPE
