@@ -131,9 +131,10 @@ q8_status check_product(bool mx4, const q8::Product& p, int64_t K)
     const struct { const void* p; int64_t bytes; } in[] = {
         {p.x, p.x_count * p.pitch}, {p.w, w_rows * p.pitch}, {p.xs, p.x_count * (p.pitch / 16)}, {p.ws, w_rows * (p.pitch / 16)},
         {p.x_rows, 4 * p.M}, {p.group_rows, 4 * (int64_t)p.n_groups}, {p.bias, 4 * w_rows}, {p.sx, 4}, {p.sw, 4 * (int64_t)p.n_groups},
-        {p.next_scale, 4}, {p.out_amax, 4}};
+        {p.next_scale, 4}};
     for (const auto& r : in)
-        if (overlap(r.p, r.bytes, p.y, y_bytes) || (ys_bytes && overlap(r.p, r.bytes, p.y_scales, ys_bytes))) return Q8_ERR_OVERLAP;
+        if (overlap(r.p, r.bytes, p.y, y_bytes) || overlap(r.p, r.bytes, p.out_amax, 4) || (ys_bytes && overlap(r.p, r.bytes, p.y_scales, ys_bytes))) return Q8_ERR_OVERLAP;
+    if (overlap(p.y, y_bytes, p.out_amax, 4)) return Q8_ERR_OVERLAP;
     if (ys_bytes && overlap(p.y, y_bytes, p.y_scales, ys_bytes)) return Q8_ERR_OVERLAP;
     return Q8_OK;
 }

@@ -52,3 +52,18 @@ def test_gradient_of_either_type_refuses(lib):
 def test_combine_refuses_rows_beyond_any_tensor(lib, N):
     for T, R, t in ((4, 0, F32), (4, 0, BF16), (1, 1, F32)):
         assert lib.q8_combine(at(0), R, at(1), at(2), T, 2, N, at(3), t, None) == SHAPE
+
+
+def test_int8_grouped_refuses_an_absmax_that_is_read(lib):
+    """The abs-max is raised while other workgroups still read the call's inputs."""
+    x, w, b, sx, sw, g, r, y, a, ns = (at(i) for i in range(10))
+    absmax, requant = 2, 4
+
+    def f(a, rows=None, ns=None, flags=absmax):
+        return lib.q8_linear_grouped(x, 4, rows, w, b, sx, sw, g, 2, 4, 8, 16, y, a, ns, flags, None)
+
+    for bad in (x + 60, w + 4, b + 4 * 15, sx, sw + 4, g + 4):
+        assert f(bad) == OVERLAP, hex(bad)
+    assert f(r + 12, rows=r) == OVERLAP
+    assert f(ns, ns=ns, flags=absmax | requant) == OVERLAP
+    assert f(y + 4 * 31) == OVERLAP
