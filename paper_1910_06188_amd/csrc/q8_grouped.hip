@@ -67,8 +67,11 @@ int launch_product(bool mx4, const Product& p, hipStream_t st)
 {
     int v = g_variant;
     if (v < 0 || v > 1 + (int)(sizeof(kTiles) / sizeof(kTiles[0]))) return 1;
-    if (v == 0) v = choose(mx4, p);
-    if (v > 1 && tile_eligible(p, kTiles[v - 2].rows)) return kTiles[v - 2].launch(mx4, p, st);
+    const bool automatic = v == 0;
+    if (automatic) v = choose(mx4, p);
+    // Rows of y too long for a tile's offsets may fit the ones of fewer rows.  So whether a launch is tiled does not hang on the tile, which depends on y's type.
+    for (; v > 1; v = automatic ? v - 1 : 1)
+        if (tile_eligible(p, kTiles[v - 2].rows)) return kTiles[v - 2].launch(mx4, p, st);
     return launch_product_direct(mx4, p, st);
 }
 

@@ -103,3 +103,33 @@ def test_a_training_step_through_the_quantizer(q8, kind):
     d = np.zeros((24, 96))
     d[3, 40], step = 1, 0.5
     assert abs((loss(host(x) + step * d) - loss(host(x) - step * d)) / (2 * step) - host(grad_x)[3, 40]) <= 1e-9
+
+
+# ---- outputs too wide for the largest tile ---------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("N", [1 << 21, (1 << 21) + 256 * 200 + 128, 1 << 22])
+def test_codes_of_a_very_wide_layer_are_those_of_its_fp32_output(q8, N):
+    """256 rows of this width reach past 31 bits of offset: outputs of every type still come from the same sums."""
+    M, K, G = 256, 8192, 64
+    g = torch.Generator(device="cuda")
+    g.manual_seed(N)
+    rand = lambda *s, lo=0, hi=256: torch.randint(lo, hi, s, generator=g, device="cuda", dtype=torch.uint8)  # noqa: E731
+    xq, wq = (rand(M, 64 * G), rand(G, M, 4, lo=112, hi=130)), (rand(N, 64 * G), rand(G, N, 4, lo=112, hi=130))      # sums that round
+    b = torch.randn(N, generator=g, device="cuda")
+    y = torch.empty((M, N), device="cuda")
+    q8.q8_mx4_linear(*xq, *wq, b, y)
+    half = torch.empty((M, N), dtype=torch.bfloat16, device="cuda")
+    q8.q8_mx4_linear(*xq, *wq, b, half)
+    assert torch.equal(half, y.bfloat16())
+    codes, scales = q8.mx4_empty(M, N)
+    q8.q8_mx4_linear(*xq, *wq, b, codes, y_scales=scales)
+    for n in range(0, N, q8.MX4_MAX_K):              # the quantizer takes rows of up to MX4_MAX_K
+        part = y[:, n: n + q8.MX4_MAX_K].contiguous()
+        want = quantized(q8, part)
+        assert torch.equal(scales[n // 128: n // 128 + len(want[1])], want[1]) and torch.equal(codes[:, n // 2: n // 2 + want[0].shape[1]], want[0])
+    # a few outputs against 64 bits
+    cols = torch.tensor([0, 1, 4095, N - 129, N - 2, N - 1], device="cuda")
+    xv, wv = MX.values(host(xq[0][:40]), host(xq[1][:, :40])), MX.values(host(wq[0][cols]), host(wq[1][:, cols]))
+    # K / 64 instructions, eight partial sums and the bias, each off by 2^-23 of the magnitudes summed at most
+    err = (K / 64 + 10) * 2.0 ** -23 * (np.abs(xv) @ np.abs(wv).T + np.abs(host(b[cols])))
+    assert (np.abs(host(y[:40][:, cols]) - (xv @ wv.T + host(b[cols]))) <= err).all()
