@@ -116,7 +116,7 @@ static int launch(const T* x, int64_t M, int64_t K, uint8_t* codes, uint8_t* sca
     const bool aligned = reinterpret_cast<uintptr_t>(x) % 16 == 0 && reinterpret_cast<uintptr_t>(xq) % 16 == 0;
     if constexpr (!kCodes) {
         const int64_t vectors = M * K / kElems;
-        if (aligned && K % 32 == 0 && vectors < (int64_t)1 << 32) {
+        if (aligned && K % 32 == 0 && vectors <= ((int64_t)1 << 32) - 64) {  // a launch is limited to 2^32 threads, less a workgroup
             hipLaunchKernelGGL(mx4_fake_quantize_kernel<T>, dim3((unsigned)((vectors + 63) / 64)), dim3(64), 0, st, x, xq, vectors);
             return hipGetLastError() == hipSuccess ? 0 : 1;
         }
@@ -125,7 +125,7 @@ static int launch(const T* x, int64_t M, int64_t K, uint8_t* codes, uint8_t* sca
     // one unit for fp32 (12288 x 4096: 39.3 us, two 40.5, four 42.5), two for bf16, whose loads are half as wide (22.3, 20.5, 21.8)
     constexpr int kWaves = 4, kUnits = sizeof(T) == 4 ? 1 : 2;
     const int64_t blocks = (M + kWaves * 4 * kUnits - 1) / (kWaves * 4 * kUnits) * groups;
-    if (blocks * kWaves * 64 >= (int64_t)1 << 32) return 1;  // a launch is limited to 2^32 threads
+    if (blocks * kWaves * 64 >= (int64_t)1 << 32) return 1;
     hipLaunchKernelGGL((mx4_quantize_kernel<T, kCodes, kWaves, kUnits>), dim3((unsigned)blocks), dim3(kWaves * 64), 0, st, x, M, K, (unsigned)groups, codes, scales, xq);
     return hipGetLastError() == hipSuccess ? 0 : 1;
 }

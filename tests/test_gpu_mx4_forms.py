@@ -133,3 +133,24 @@ def test_codes_of_a_very_wide_layer_are_those_of_its_fp32_output(q8, N):
     # K / 64 instructions, eight partial sums and the bias, each off by 2^-23 of the magnitudes summed at most
     err = (K / 64 + 10) * 2.0 ** -23 * (np.abs(xv) @ np.abs(wv).T + np.abs(host(b[cols])))
     assert (np.abs(host(y[:40][:, cols]) - (xv @ wv.T + host(b[cols]))) <= err).all()
+
+
+def test_fake_quantize_of_as_many_vectors_as_a_launch_has_threads(q8):
+    """69 GB of fp32: 2^32 - 8 vectors of 16 bytes, which in workgroups of 64 are 2^32 threads, one more than a launch takes."""
+    M, K = 256999, 66848
+    assert M * K // 4 == (1 << 32) - 8
+    if torch.cuda.mem_get_info()[0] + torch.cuda.memory_reserved() < 80 << 30:
+        pytest.skip("needs 69 GB")
+    torch.cuda.empty_cache()
+    x = torch.zeros((M, K), device="cuda")
+    ends = [slice(0, 20), slice(M - 20, M)]
+    want = []
+    for s in ends:
+        x[s] = torch.randn(20, K, device="cuda")
+        want.append(MX.values(*MX.quantize(host(x[s])), K))
+    q8.q8_mx4_fake_quantize(x, x)
+    for s, v in zip(ends, want):
+        np.testing.assert_array_equal(host(x[s]), v)
+    assert not x[20:2000].any() and not x[M - 2000: M - 20].any()
+    del x
+    torch.cuda.empty_cache()
