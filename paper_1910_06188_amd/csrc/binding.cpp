@@ -145,7 +145,14 @@ int float_type(const at::Tensor& t, const char* where)
 }
 void* float_data(const at::Tensor& t, const char* where) { return address(t, t.scalar_type(), where); }
 
-uint32_t flags_of(PyObject* o) { return static_cast<uint32_t>(PyLong_AsUnsignedLongMask(o)); }
+struct Pending {};  // a Python error is set
+
+uint32_t flags_of(PyObject* o)
+{
+    const uint32_t flags = static_cast<uint32_t>(PyLong_AsUnsignedLongMask(o));
+    if (PyErr_Occurred()) throw Pending{};
+    return flags;
+}
 
 // Codes [.., rows, 64 G] and scales [.., G, rows, 4], `dims` dimensions of codes.
 void check_mx4(const at::Tensor& codes, const at::Tensor& scales, int64_t dims, const char* where)
@@ -366,9 +373,13 @@ template <class Entry>
 PyObject* checked(PyObject*, PyObject* const* args, Py_ssize_t n)
 {
     if (n != Entry::kArgs) return PyErr_Format(PyExc_TypeError, "takes %d arguments, got %zd", Entry::kArgs, n);
+    if (args[n - 1] != Py_None) {  // no launch on what is no handle
+        stream_of(args[n - 1]);
+        if (PyErr_Occurred()) return nullptr;
+    }
     try {
-        const q8_status status = Entry::run(args, Name<Entry>::kText);
-        return PyErr_Occurred() ? nullptr : PyLong_FromLong(static_cast<long>(status));
+        return PyLong_FromLong(static_cast<long>(Entry::run(args, Name<Entry>::kText)));
+    } catch (const Pending&) {
     } catch (const Refused& r) {
         PyErr_SetString(r.type, r.text.c_str());
     } catch (const std::exception& e) {  // a tensor without storage of its own (under a functional transform)

@@ -67,3 +67,26 @@ def test_int8_grouped_refuses_an_absmax_that_is_read(lib):
     assert f(r + 12, rows=r) == OVERLAP
     assert f(ns, ns=ns, flags=absmax | requant) == OVERLAP
     assert f(y + 4 * 31) == OVERLAP
+
+
+def test_native_entry_points_refuse_what_is_no_stream_before_all_else():
+    import torch
+    from paper_1910_06188_amd import _binding, q8
+    x = torch.zeros(4, 128)
+    c, s = q8.mx4_empty(4, 128, device="cpu")
+    n = torch.zeros(4, dtype=torch.int32)
+    calls = {
+        "q8_mx4_quantize": (x, c, s), "q8_mx4_fake_quantize": (x, x.clone()), "q8_mx4_ste_backward": (x, x.clone()), "q8_mx4_linear": (c, s, c, s, None, x, None, 0),
+        "q8_mx4_linear_dynamic": (x, c, s, None, c, s, x, None, 0), "q8_mx4_linear_grouped": (c, s, c[None], s[None], None, n[:1], x, None, None, 0),
+        "q8_linear_grouped": (x.char(), x.char()[None], None, x, x[0, :1], n[:1], x[:, :4], None, None, None, 0), "q8_route": (x, n.view(4, 1), x[:, :1], n, n, n, n),
+        "q8_combine": (x, n.view(4, 1), x[:, :1], x),
+    }
+    for name, args in calls.items():
+        f = getattr(_binding, name)
+        for bad in ("stream", 1.5, x):
+            with pytest.raises(TypeError):
+                f(*args, bad)
+        with pytest.raises(TypeError, match="arguments"):
+            f(*args)
+        with pytest.raises(ValueError):
+            f(*args, 0)
