@@ -66,16 +66,28 @@ __device__ __forceinline__ float dequant_factor(float sx, float sw)
 // side and one rounding of the result on the positive side, a twentieth of the tolerance the
 // tests allow; beyond 6 the term is below 6e-9 and |v| is clamped.  Nine VALU operations and
 // one transcendental per element.
+// kNan: a NaN for a NaN.  Its two comparisons are the ones that pass a NaN on, which also spares the compiler the operation that quiets their operands.
+template <bool kNan>
+__device__ __forceinline__ float smaller(float a, float b)
+{
+    return kNan ? __builtin_elementwise_minimum(a, b) : __builtin_fminf(a, b);
+}
+template <bool kNan>
+__device__ __forceinline__ float larger(float a, float b)
+{
+    return kNan ? __builtin_elementwise_maximum(a, b) : __builtin_fmaxf(a, b);
+}
+template <bool kNan = false>
 __device__ __forceinline__ float gelu_erf(float v)
 {
-    const float a = __builtin_fminf(__builtin_fabsf(v), 6.0f);
+    const float a = smaller<kNan>(__builtin_fabsf(v), 6.0f);
     float p = __builtin_fmaf(3.309277963e-05f, a, -7.692193612e-04f);
     p = __builtin_fmaf(p, a, 8.080715314e-03f);
     p = __builtin_fmaf(p, a, -5.341210216e-02f);
     p = __builtin_fmaf(p, a, -4.587709606e-01f);
     p = __builtin_fmaf(p, a, -1.151201725e+00f);
     p = __builtin_fmaf(p, a, -9.999930859e-01f);
-    return __builtin_fmaf(-a, __builtin_amdgcn_exp2f(p), __builtin_fmaxf(v, 0.0f));  // one rounding, one operation less
+    return __builtin_fmaf(-a, __builtin_amdgcn_exp2f(p), larger<kNan>(v, 0.0f));  // one rounding, one operation less
 }
 
 // Maximum over the 64 lanes, the same value in every lane: a scan inside each row of 16 lanes with DPP row shifts (lanes

@@ -152,7 +152,7 @@ __device__ __forceinline__ float product_value(typename Op::Sum sum, const Produ
 template <class Op>
 __device__ __forceinline__ float product_gelu(float v)
 {
-    return Op::kMx4 ? gelu_erf_nan(v) : gelu_erf(v);
+    return gelu_erf<Op::kMx4>(v);
 }
 
 // Maximum over each half of 32 lanes.

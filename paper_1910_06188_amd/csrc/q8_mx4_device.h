@@ -72,20 +72,6 @@ __device__ __forceinline__ unsigned f32_to_bf16x2(float low, float high)
 }
 __device__ __forceinline__ unsigned short f32_to_bf16(float f) { return __builtin_bit_cast(unsigned short, (__bf16)f); }
 
-// gelu_erf (q8_device.h) with a NaN for a NaN: the same polynomial and roundings, but the two comparisons are the ones that pass a NaN on,
-// which also spares the compiler the operation that quiets their operands.
-__device__ __forceinline__ float gelu_erf_nan(float v)
-{
-    const float a = __builtin_elementwise_minimum(__builtin_fabsf(v), 6.0f);
-    float p = __builtin_fmaf(3.309277963e-05f, a, -7.692193612e-04f);
-    p = __builtin_fmaf(p, a, 8.080715314e-03f);
-    p = __builtin_fmaf(p, a, -5.341210216e-02f);
-    p = __builtin_fmaf(p, a, -4.587709606e-01f);
-    p = __builtin_fmaf(p, a, -1.151201725e+00f);
-    p = __builtin_fmaf(p, a, -9.999930859e-01f);
-    return __builtin_fmaf(-a, __builtin_amdgcn_exp2f(p), __builtin_elementwise_maximum(v, 0.0f));
-}
-
 // The first `left` (at most eight) of eight elements at whatever address, zeros behind them.
 __device__ __forceinline__ void load8(const float* p, int left, float* v)
 {

@@ -90,3 +90,11 @@ def test_native_entry_points_refuse_what_is_no_stream_before_all_else():
             f(*args)
         with pytest.raises(ValueError):
             f(*args, 0)
+
+
+def test_the_gelu_polynomial_is_written_once():
+    """The constants that test_host_logic.py checks are the ones of every kernel."""
+    csrc = os.path.join(ROOT, "paper_1910_06188_amd", "csrc")
+    text = "".join(open(os.path.join(csrc, f)).read() for f in sorted(os.listdir(csrc)))
+    for constant in ("3.309277963e-05f", "9.999930859e-01f"):
+        assert text.count(constant) == 1
