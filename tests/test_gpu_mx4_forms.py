@@ -154,3 +154,183 @@ def test_fake_quantize_of_as_many_vectors_as_a_launch_has_threads(q8):
     assert not x[20:2000].any() and not x[M - 2000: M - 20].any()
     del x
     torch.cuda.empty_cache()
+
+
+# ---- layers quantized on the way ---------------------------------------------------------------------------------------------
+
+def gelu_and_tolerance(ref, mag, K, gelu):
+    """Of fp32 outputs: K / 64 matrix instructions, eight partial sums and a bias, each off by 2^-23 of the magnitudes summed at most (an instruction may
+    truncate); GELU's slope is at most 1.13, its own error 5.2e-7 and a rounding."""
+    err = (K / 64 + 10) * 2.0 ** -23 * mag
+    return (MX.gelu(ref), 1.13 * err + 5.2e-7 + 2.0 ** -23 * np.abs(ref)) if gelu else (ref, err)
+
+
+def activations(g, M, K):
+    return (g.standard_normal((M, K)) * np.exp(0.5 * g.standard_normal((M, 1))) * np.exp(g.standard_normal((1, K)))).astype(np.float32)
+
+
+# One launch up to min(M, 32) K = 24576, K = 4096 and 512 tiles of 32 x 32; both sides of each, and odd sizes.
+DYNAMIC = [(1, 1024, 4096), (1, 1, 1), (3, 333, 256), (2, 33, 129), (7, 129, 70), (16, 768, 768), (24, 1024, 256), (25, 1024, 256), (31, 127, 33), (32, 768, 130), (33, 768, 130), (32, 769, 128),
+           (5, 4096, 128), (5, 4097, 128), (6, 4096, 96), (32, 768, 16384), (32, 768, 16385), (512, 512, 1024), (513, 512, 1024), (300, 100, 384)]
+
+
+@pytest.mark.parametrize("M,K,N", DYNAMIC)
+@pytest.mark.parametrize("kind", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("gelu", [False, True])
+@pytest.mark.parametrize("offset", [0, 1])
+def test_dynamic_layer_of_either_type(q8, M, K, N, kind, gelu, offset):
+    g = np.random.default_rng(M + K + N)
+    room = torch.zeros(offset + M * K, dtype=kind, device="cuda")
+    x = room[offset:].view(M, K)
+    x.copy_(dev(activations(g, M, K)).to(kind))
+    wq, b = quantized(q8, dev(activations(g, N, K))), dev(g.standard_normal(N).astype(np.float32))
+    flags = q8.EPI_GELU if gelu else 0
+    work = q8.mx4_empty(M, K)
+    work[0].fill_(0xFF), work[1].fill_(0xFF)
+
+    def layer(y, y_scales=None, bias=b):
+        q8.q8_mx4_linear_dynamic(x, *wq, bias, *work, y, y_scales=y_scales, flags=flags)
+        return y
+
+    y = layer(torch.full((M, N), 7.0, device="cuda"))
+    xv, wv = MX.values(*MX.quantize(host(x)), K), MX.values(host(wq[0]), host(wq[1]), K)
+    ref, err = gelu_and_tolerance(*MX.grouped(xv, [wv], [host(b)], [M], M), K, gelu)
+    assert (np.abs(host(y) - ref) <= err).all()
+    assert torch.equal(layer(torch.full((M, N), 7.0, dtype=torch.bfloat16, device="cuda")), y.bfloat16())       # one rounding of the same sums
+    bare = layer(torch.full((M, N), 7.0, device="cuda"), bias=None)
+    ref, err = gelu_and_tolerance(*MX.grouped(xv, [wv], None, [M], M), K, gelu)
+    assert (np.abs(host(bare) - ref) <= err).all()
+    if N % 128 == 0:
+        want, (codes, scales) = quantized(q8, y), q8.mx4_empty(M, N)
+        codes.fill_(0xA5), scales.fill_(0x5A)
+        layer(codes, scales)
+        assert torch.equal(scales, want[1]) and torch.equal(codes, want[0])
+
+
+@pytest.mark.parametrize("M,K", [(5, 300), (6, 4096), (24, 1024), (200, 1024)])
+@pytest.mark.parametrize("kind", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("gelu", [False, True])
+def test_dynamic_layer_follows_nan_and_infinity(q8, M, K, kind, gelu):
+    """A block of x with an infinity or a NaN makes its row NaN, one of w its column; nothing else changes."""
+    g = np.random.default_rng(M + K)
+    N = 256
+    x, w = activations(g, M, K), activations(g, N, K)
+    b = g.standard_normal(N).astype(np.float32)
+    x[1, 40], x[3, K - 1], x[4, 0] = np.nan, np.inf, -np.inf
+    x[2] = 0                                          # a row of zeros gives the bias
+    w[7, 0], w[130, K - 1] = -np.inf, np.nan
+    x, wq = dev(x).to(kind), quantized(q8, dev(w))
+    flags = q8.EPI_GELU if gelu else 0
+    y = torch.full((M, N), 7.0, device="cuda")
+    q8.q8_mx4_linear_dynamic(x, *wq, dev(b), *q8.mx4_empty(M, K), y, flags=flags)
+    want = np.zeros((M, N), bool)
+    want[[1, 3, 4]], want[:, [7, 130]] = True, True
+    np.testing.assert_array_equal(np.isnan(host(y)), want)
+    with np.errstate(invalid="ignore"):
+        xv, wv = np.nan_to_num(MX.values(*MX.quantize(host(x)), K)), np.nan_to_num(MX.values(host(wq[0]), host(wq[1]), K))
+    ref, err = gelu_and_tolerance(*MX.grouped(xv, [wv], [b], [M], M), K, gelu)
+    assert (np.abs(host(y) - ref) <= err)[~want].all()
+    codes, scales = q8.mx4_empty(M, N)
+    q8.q8_mx4_linear_dynamic(x, *wq, dev(b), *q8.mx4_empty(M, K), codes, y_scales=scales, flags=flags)
+    expect = quantized(q8, y)
+    assert torch.equal(scales, expect[1]) and torch.equal(codes, expect[0])
+    block = want.reshape(M, N // 32, 32).any(-1)      # blocks of 32 columns with a NaN
+    np.testing.assert_array_equal(host(scales).transpose(1, 0, 2).reshape(M, N // 32) == 255, block)
+
+
+@pytest.mark.parametrize("M,K,N", [(4, 1024, 512), (200, 1000, 520)])
+def test_dynamic_layer_captured_and_replayed(q8, M, K, N):
+    """One launch and two in a graph, replayed on new activations between eager calls that share nothing with it."""
+    g = np.random.default_rng(M)
+    wq, b = quantized(q8, dev(activations(g, N, K))), dev(g.standard_normal(N).astype(np.float32))
+    x, y, work = torch.zeros((M, K), dtype=torch.bfloat16, device="cuda"), torch.zeros((M, N), dtype=torch.bfloat16, device="cuda"), q8.mx4_empty(M, K)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        q8.q8_mx4_linear_dynamic(x, *wq, b, *work, y, flags=q8.EPI_GELU)
+    for i in range(5):
+        x.copy_(dev(activations(np.random.default_rng(i), M, K)))
+        want = torch.empty_like(y)
+        q8.q8_mx4_linear_dynamic(x, *wq, b, *q8.mx4_empty(M, K), want, flags=q8.EPI_GELU)
+        torch.cuda.synchronize()
+        y.fill_(7), work[0].fill_(0xFF), work[1].fill_(0xFF)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(y, want), i
+
+
+# ---- a mixture of experts on int8 codes ---------------------------------------------------------------------------------------
+
+class Int8Moe:
+    """As a program runs it: route, quantize, first layer with GELU to the next layer's codes and their abs-max, second layer, combine."""
+
+    def __init__(self, q8, T, E, k, H, F, room=0):
+        g = np.random.default_rng(T + E)
+        self.q8, self.sizes, R = q8, (T, E, k, H, F), T * k + room
+        i32, f32, i8 = (dict(dtype=t, device="cuda") for t in (torch.int32, torch.float32, torch.int8))
+        self.x, self.logits = torch.empty((T, H), **f32), torch.empty((T, E), **f32)
+        self.w1, self.w2 = dev(g.integers(-127, 128, (E, F, H)).astype(np.int8)), dev(g.integers(-127, 128, (E, H, F)).astype(np.int8))
+        self.s1, self.s2 = (dev((127 / (n ** -0.5) * (0.5 + g.random(E))).astype(np.float32)) for n in (H, F))
+        self.b1, self.b2 = dev(g.standard_normal((E, F)).astype(np.float32)), dev(g.standard_normal((E, H)).astype(np.float32))
+        self.sx, self.sh, self.amax, self.h_amax = (torch.zeros(1, **f32) for _ in range(4))
+        self.sh.fill_(20.0)
+        self.experts, self.slots, self.counts, self.work = torch.empty((T, k), **i32), torch.empty((T, k), **i32), torch.empty(E, **i32), torch.empty(q8.ROUTE_BLOCKS * E, **i32)
+        self.rows, self.gates = torch.zeros(R, **i32), torch.empty((T, k), **f32)
+        self.xq, self.h, self.y, self.out = torch.empty((T, H), **i8), torch.zeros((R, F), **i8), torch.zeros((R, H), **f32), torch.zeros((T, H), **f32)
+        self.fill(0)
+
+    def fill(self, seed):
+        g, (T, E, k, H, F) = np.random.default_rng(seed), self.sizes
+        self.x.copy_(dev(g.standard_normal((T, H)).astype(np.float32))), self.logits.copy_(dev(g.standard_normal((T, E)).astype(np.float32)))
+
+    def run(self, stream=None):
+        q8, (T, E, k, H, F) = self.q8, self.sizes
+        q8.q8_route(self.logits, self.experts, self.gates, self.counts, self.rows[: T * k], self.slots, self.work, stream=stream)
+        q8.q8_absmax(self.x, self.amax, self.sx, stream=stream)
+        q8.q8_quantize(self.x, self.sx, self.xq, stream=stream)
+        q8.q8_linear_grouped(self.xq, self.w1, self.b1, self.sx, self.s1, self.counts, self.h, x_rows=self.rows, out_amax=self.h_amax, next_scale=self.sh,
+                             flags=q8.EPI_GELU | q8.EPI_REQUANT | q8.EPI_ABSMAX, stream=stream)
+        q8.q8_linear_grouped(self.h, self.w2, self.b2, self.sh, self.s2, self.counts, self.y, stream=stream)
+        q8.q8_combine(self.y, self.slots, self.gates, self.out, stream=stream)
+        return self.out
+
+
+@pytest.mark.parametrize("T,E,k,H,F,room", [(1, 4, 2, 128, 256, 0), (33, 8, 2, 200, 384, 5), (100, 8, 2, 1024, 512, 56), (700, 6, 3, 256, 512, 40), (3000, 2, 1, 256, 256, 0)])
+def test_int8_mixture_of_experts(q8, T, E, k, H, F, room):
+    """The layers bit for bit as q8_linear has each expert's rows; rows behind the last expert's as they were."""
+    m = Int8Moe(q8, T, E, k, H, F, room)
+    R = T * k
+    m.h.fill_(9), m.y.fill_(9)
+    m.run()
+    experts, gates, counts, rows, slots = MX.route(host(m.logits).astype(np.float32), k)
+    for got, want in ((m.experts, experts), (m.counts, counts), (m.rows[:R], rows), (m.slots, slots)):
+        np.testing.assert_array_equal(host(got), want)
+    h, y, amax = torch.full_like(m.h, 9), torch.full_like(m.y, 9), torch.zeros(1, device="cuda")
+    mine = m.xq[m.rows[:R].long()]
+    for e, (a, z) in enumerate(MX.spans(counts, R)):
+        if z > a:
+            q8.q8_linear(mine[a:z].contiguous(), m.w1[e], m.b1[e], m.sx, m.s1[e: e + 1], h[a:z], out_amax=amax, next_scale=m.sh, flags=q8.EPI_GELU | q8.EPI_REQUANT | q8.EPI_ABSMAX)
+            q8.q8_linear(h[a:z], m.w2[e], m.b2[e], m.sh, m.s2[e: e + 1], y[a:z])
+    assert torch.equal(m.h, h) and torch.equal(m.y, y) and torch.equal(m.h_amax, amax)
+    assert float(h[:R].float().abs().mean()) > 1      # the codes are in use
+    terms = host(m.gates)[..., None] * host(m.y)[slots]
+    err = k * 2.0 ** -24 * 1.001 * np.abs(terms).sum(1)        # k fused additions, each rounded once
+    assert (np.abs(host(m.out) - terms.sum(1)) <= err).all()
+
+
+def test_int8_mixture_of_experts_captured_and_replayed(q8):
+    m = Int8Moe(q8, 150, 8, 2, 256, 512, room=10)
+    m.run()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        m.run()
+    for i in range(5):
+        m.fill(i + 1)
+        m.h_amax.zero_()
+        want = m.run().clone(), m.h_amax.clone()
+        torch.cuda.synchronize()
+        m.out.zero_(), m.counts.zero_(), m.work.fill_(3), m.h_amax.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(m.out, want[0]) and torch.equal(m.h_amax, want[1]), i
