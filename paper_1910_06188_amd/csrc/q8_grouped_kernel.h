@@ -457,11 +457,9 @@ int launch_product_tile(const Product& p, hipStream_t st)
     const int64_t tiles_n = (p.N + BN - 1) / BN, tiles = row_tiles(p.M, p.n_groups, BM) * tiles_n;
     if (tiles * WGM * WGN * 64 >= (int64_t)1 << 32) return 1;
     const dim3 grid((unsigned)tiles), block(WGM * WGN * 64);
-    // What the next layer reads may wait for it in the Infinity Cache (256 MB); only outputs that do not fit there are stored past the caches.  K = 1024, N = 4096 and
-    // the quantizer of the next layer behind it, us, without and with: 96 MB of fp32 44.3 and 47.1, 192 MB 77.1 and 88.3, 224 MB 100.8 and 101.4, 240 MB 110.4 and
-    // 105.8, 320 MB 176.5 and 148.4; 48 MB of bf16 36.2 and 36.3, 96 MB 59.3 and 62.0, 160 MB 93.1 and 97.9.  The product by itself, over and over: 64 MB of fp32
-    // 20.3 and 20.1, 192 MB 47.2 and 48.0, 320 MB 87.2 and 75.2; 32 MB of bf16 16.4 and 15.0, 96 MB 39.1 and 36.8.
-    const int stream_out = p.M * p.N * (p.y_type == Q8_TYPE_BF16 ? 2 : 4) >= (int64_t)224 << 20;
+    // Outputs that the L2s (32 MB together) do not hold anyway are stored past them: 12288 x 4096 -> 1024 to fp32 33.4 us without, 31.9 with; 12288 x 1024 -> 4096 to
+    // bf16 42.6 and 41.0, to fp32 47.0 and 48.2.
+    const int stream_out = p.M * p.N * (p.y_type == Q8_TYPE_BF16 ? 2 : 4) >= (int64_t)32 << 20;
 #define Q8_PT_LAUNCH(OUT) \
     hipLaunchKernelGGL((product_tile_kernel<Op, BM, BN, WGM, WGN, kSlots, kAhead, kWgs, OUT>), grid, block, 0, st, p, (unsigned)tiles_n, (unsigned)(((int64_t)1 << 32) / (kPanel * tiles_n)), stream_out)
     if (p.y_type == Q8_TYPE_F32) {
