@@ -457,8 +457,11 @@ int launch_product_tile(const Product& p, hipStream_t st)
     const int64_t tiles_n = (p.N + BN - 1) / BN, tiles = row_tiles(p.M, p.n_groups, BM) * tiles_n;
     if (tiles * WGM * WGN * 64 >= (int64_t)1 << 32) return 1;
     const dim3 grid((unsigned)tiles), block(WGM * WGN * 64);
-    // Outputs that the L2s (32 MB together) do not hold anyway are stored past them: 12288 x 4096 -> 1024 to fp32 33.4 us without, 31.9 with; 12288 x 1024 -> 4096 to
-    // bf16 42.6 and 41.0, to fp32 47.0 and 48.2.
+    // Outputs that the L2s (32 MB together) do not hold anyway are stored past the caches: lying dirty in the 256 MB behind the L2s, they are written back under the
+    // next launch.  K = 1024, N = 4096, us, with ordinary stores and with these, four sets of tensors in turn, as the layers of a model have them: 96 MB of fp32 31.8 and
+    // 27.5, 192 MB 56.3 and 48.2, 320 MB 88.2 and 76.1; 48 MB of bf16 23.4 and 21.7, 128 MB 62.4 and 51.8.  With the next layer's quantizer behind each: 47.5
+    // and 51.1, 96.2 and 95.2, 165.1 and 153.9; 36.8 and 36.1, 91.8 and 95.2.  The other way round only where all of it stays in the caches: one set, 192 MB with the
+    // quantizer 77.2 and 87.0, by itself 47.7 and 47.8.
     const int stream_out = p.M * p.N * (p.y_type == Q8_TYPE_BF16 ? 2 : 4) >= (int64_t)32 << 20;
 #define Q8_PT_LAUNCH(OUT) \
     hipLaunchKernelGGL((product_tile_kernel<Op, BM, BN, WGM, WGN, kSlots, kAhead, kWgs, OUT>), grid, block, 0, st, p, (unsigned)tiles_n, (unsigned)(((int64_t)1 << 32) / (kPanel * tiles_n)), stream_out)

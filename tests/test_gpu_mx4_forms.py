@@ -334,3 +334,24 @@ def test_int8_mixture_of_experts_captured_and_replayed(q8):
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(m.out, want[0]) and torch.equal(m.h_amax, want[1]), i
+
+
+@pytest.mark.parametrize("v", [2, 3, 4, 5])
+@pytest.mark.parametrize("M", [1000, 1050, 2000, 2100])
+def test_outputs_stored_for_the_caches_and_past_them(q8, v, M):
+    """Outputs of either type on both sides of 32 MiB are the same numbers in every tile: those of the layer's rows taken a few at a time."""
+    N, K = 8200, 256
+    g = np.random.default_rng(M)
+    xq, wq, b = quantized(q8, dev(activations(g, M, K))), quantized(q8, dev(activations(g, N, K))), dev(g.standard_normal(N).astype(np.float32))
+    y, half = torch.full((M, N), 7.0, device="cuda"), torch.full((M, N), 7.0, dtype=torch.bfloat16, device="cuda")
+    q8.set_product_variant(v)
+    try:
+        q8.q8_mx4_linear(*xq, *wq, b, y)
+        q8.q8_mx4_linear(*xq, *wq, b, half)
+        part = torch.empty((300, N), device="cuda")
+        for m in (0, 500, M - 300):
+            q8.q8_mx4_linear(xq[0][m: m + 300], xq[1][:, m: m + 300].contiguous(), *wq, b, part)
+            assert torch.equal(part, y[m: m + 300])
+    finally:
+        q8.set_product_variant(0)
+    assert torch.equal(half, y.bfloat16())
