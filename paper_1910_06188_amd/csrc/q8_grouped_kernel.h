@@ -171,7 +171,7 @@ __global__ __launch_bounds__(WGM* WGN * 64, kWgs* WGM* WGN / 4) void product_til
     };
 
     const int wm = wave / WGN, wn = wave % WGN;
-    const auto column = [&](int j) { return kPairs ? j / 2 * 64 + 2 * l32 + j % 2 : j * 32 + l32; };  // of the wave's, this lane's of block j if it has one
+    const auto column_of = [](int j, int l) { return kPairs ? j / 2 * 64 + 2 * l + j % 2 : j * 32 + l; };  // of the wave's, lane l's of block j if it has one
     // Where this lane finds its 16 bytes of step 0 in the first block of its wave's rows.  32 rows on, a row's swizzle differs in bit 2 alone,
     // so the block behind is 4 KiB away and the chunk's bit flipped; step ks has ks in the chunk's low bits.  So neither needs an address of its own: the
     // registers that eight of them took keep 128x128 tiles from having four workgroups a unit (24576 rows of 16 experts, 1024 -> 4096 92 us with three, 84 with
@@ -208,7 +208,7 @@ __global__ __launch_bounds__(WGM* WGN * 64, kWgs* WGM* WGN / 4) void product_til
                     for (int e = 0; e < 4; ++e) acc[i][j][4 * q + e] = c[e];
             }
         } else {
-            const Sum c = Op::kMx4 ? 0 : bias[wn * TN + column(j)];
+            const Sum c = Op::kMx4 ? 0 : bias[wn * TN + column_of(j, l32)];
 #pragma unroll
             for (int i = 0; i < FM; ++i)
 #pragma unroll
@@ -281,7 +281,9 @@ __global__ __launch_bounds__(WGM* WGN * 64, kWgs* WGM* WGN / 4) void product_til
 
     __builtin_amdgcn_s_setprio(0);
 
-    // Epilogue.
+    // Epilogue.  The lane's number is counted anew, so that it takes no register through the loop.
+    const int out_lane = (int)__builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0)), out_l32 = out_lane & 31, out_hi = out_lane >> 5;
+    const auto column = [&](int j) { return column_of(j, out_l32); };
     typedef unsigned v2u __attribute__((ext_vector_type(2)));
     typedef unsigned v4u __attribute__((ext_vector_type(4)));
     const bool gelu = p.flags & Q8_EPI_GELU;
@@ -296,7 +298,7 @@ __global__ __launch_bounds__(WGM* WGN * 64, kWgs* WGM* WGN / 4) void product_til
         if constexpr (Op::kMx4 && kRowLane) {
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
-                const v4s c = *reinterpret_cast<const v4s*>(bias + wn * TN + j * 32 + 8 * q + 4 * hi);
+                const v4s c = *reinterpret_cast<const v4s*>(bias + wn * TN + j * 32 + 8 * q + 4 * out_hi);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) v[4 * q + e] = __fadd_rn(acc[i][j][4 * q + e], c[e]);
             }
@@ -316,7 +318,7 @@ __global__ __launch_bounds__(WGM* WGN * 64, kWgs* WGM* WGN / 4) void product_til
             if (p.flags & Q8_EPI_ABSMAX) {
 #pragma unroll
                 for (int e = 0; e < 16; ++e) {
-                    const int along = 8 * (e >> 2) + 4 * hi + (e & 3), m = wm * TM + i * 32 + (kRowLane ? l32 : along), n = n0 + wn * TN + (kRowLane ? j * 32 + along : column(j));
+                    const int along = 8 * (e >> 2) + 4 * out_hi + (e & 3), m = wm * TM + i * 32 + (kRowLane ? out_l32 : along), n = n0 + wn * TN + (kRowLane ? j * 32 + along : column(j));
                     if (m < tile.rows && n < N) famax = __builtin_fmaxf(famax, __builtin_fabsf(v[e]));
                 }
             }
@@ -327,7 +329,7 @@ __global__ __launch_bounds__(WGM* WGN * 64, kWgs* WGM* WGN / 4) void product_til
         constexpr int kPair = FN < 2 ? 1 : 2;  // blocks that one store takes
 #pragma unroll
         for (int i = 0; i < FM; ++i) {
-            const int m = wm * TM + i * 32 + l32;
+            const int m = wm * TM + i * 32 + out_l32;
             const unsigned row_at = m < tile.rows ? (unsigned)(m * row_bytes) : kOutOfRange;
             const int nw = n0 + wn * TN;
             if (nw >= N) break;  // columns come in whole groups of 128
@@ -353,13 +355,13 @@ __global__ __launch_bounds__(WGM* WGN * 64, kWgs* WGM* WGN / 4) void product_til
                 if constexpr (kPair == 2) {
                     const v2u p0 = __builtin_amdgcn_permlane32_swap(c[0][0], c[1][0], false, false), p1 = __builtin_amdgcn_permlane32_swap(c[0][1], c[1][1], false, false);
                     const v4u w = {(p0[0] & 0xffffu) | (p0[1] << 16), (p0[0] >> 16) | (p0[1] & 0xffff0000u), (p1[0] & 0xffffu) | (p1[1] << 16), (p1[0] >> 16) | (p1[1] & 0xffff0000u)};
-                    __builtin_amdgcn_raw_buffer_store_b128(w, ry, row_at + (unsigned)((nw + (j + hi) * 32) / 2), 0, 0);
+                    __builtin_amdgcn_raw_buffer_store_b128(w, ry, row_at + (unsigned)((nw + (j + out_hi) * 32) / 2), 0, 0);
                 } else {
                     const v2u p0 = __builtin_amdgcn_permlane32_swap(c[0][0], c[0][1], false, false);
-                    __builtin_amdgcn_raw_buffer_store_b64(v2u{(p0[0] & 0xffffu) | (p0[1] << 16), (p0[0] >> 16) | (p0[1] & 0xffff0000u)}, ry, row_at + (unsigned)((nw + j * 32) / 2 + 8 * hi), 0, 0);
+                    __builtin_amdgcn_raw_buffer_store_b64(v2u{(p0[0] & 0xffffu) | (p0[1] << 16), (p0[0] >> 16) | (p0[1] & 0xffff0000u)}, ry, row_at + (unsigned)((nw + j * 32) / 2 + 8 * out_hi), 0, 0);
                 }
             }
-            if (hi == 0 && m < tile.rows) {
+            if (out_hi == 0 && m < tile.rows) {
                 uint8_t* s = p.y_scales + ((int64_t)(nw / kMxGroup) * p.M + tile.row + m) * 4 + (nw % kMxGroup) / 32;
                 if constexpr (FN == 4)
                     *reinterpret_cast<unsigned*>(s) = bytes;
@@ -373,7 +375,7 @@ __global__ __launch_bounds__(WGM* WGN * 64, kWgs* WGM* WGN / 4) void product_til
         const bool wide = N % 4 == 0 && reinterpret_cast<uintptr_t>(p.y) % 4 == 0;  // four codes start on a word and no row ends inside them
 #pragma unroll
         for (int i = 0; i < FM; ++i) {
-            const int m = wm * TM + i * 32 + l32;
+            const int m = wm * TM + i * 32 + out_l32;
             const unsigned row_at = m < tile.rows ? (unsigned)(m * row_bytes) : kOutOfRange;
 #pragma unroll
             for (int j = 0; j < FN; ++j) {
@@ -381,7 +383,7 @@ __global__ __launch_bounds__(WGM* WGN * 64, kWgs* WGM* WGN / 4) void product_til
                 block_values(i, j, v);
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
-                    const int n = n0 + wn * TN + j * 32 + 8 * q + 4 * hi;
+                    const int n = n0 + wn * TN + j * 32 + 8 * q + 4 * out_hi;
                     unsigned code[4];
 #pragma unroll
                     for (int e = 0; e < 4; ++e) code[e] = (unsigned)quantize_code(v[4 * q + e], next_scale) & 0xffu;
@@ -413,7 +415,7 @@ __global__ __launch_bounds__(WGM* WGN * 64, kWgs* WGM* WGN / 4) void product_til
 #pragma unroll
             for (int j = 0; j < FN; j += kStep) {
                 const int n = n0 + wn * TN + column(j);
-                const unsigned at = n < N ? (unsigned)(4 * hi * row_bytes + n * kSize) : kOutOfRange, beside = n + 1 < N ? at + kSize : kOutOfRange;
+                const unsigned at = n < N ? (unsigned)(4 * out_hi * row_bytes + n * kSize) : kOutOfRange, beside = n + 1 < N ? at + kSize : kOutOfRange;
 #pragma unroll
                 for (int i = 0; i < FM; ++i) {
                     const int m = wm * TM + i * 32;
