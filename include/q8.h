@@ -378,7 +378,8 @@ q8_status q8_attention(const float* qkv, int64_t B, int64_t S, int heads, int d,
  *                                rows lie side by side, as the matrix instructions take them.
  * Codes have to be 16-byte aligned, scales 4-byte.  Weights [N, K] are quantized along K like activations; several matrices of
  * the same shape (experts) are stored one behind the other: codes [n, N, 64 G], scales [n, G, N, 4].
- * Outputs may not overlap inputs (Q8_ERR_OVERLAP) unless stated.  NaN and infinities in inputs are followed through these calls.
+ * Outputs may not overlap inputs or each other (Q8_ERR_OVERLAP) unless stated.  NaN and infinities in the inputs of the 4-bit calls and of q8_combine come out as
+ * IEEE arithmetic has them; q8_linear_grouped treats them as q8_linear does.
  */
 #define Q8_MX4_MAX_K 1048576
 #define Q8_MX4_CODE_BYTES(K) (((int64_t)(K) + 127) / 128 * 64)   /* a row's codes */
@@ -453,7 +454,7 @@ q8_status q8_mx4_linear_grouped(const uint8_t* xq, const uint8_t* xs, int64_t x_
  * The same on int8 codes: each expert's rows as q8_linear has them, with the expert's own weights, scale and bias (one group of columns).
  *   xq int8[x_count, K]; wq int8[n_experts, N, K]; bias fp32[n_experts, N] or NULL; sx fp32[1]; sw fp32[n_experts].
  *   y fp32[M,N], or int8[M,N] with Q8_EPI_REQUANT; out_amax, next_scale and flags as q8_linear (the abs-max is that of the rows that
- *   belong to an expert).  x_count, x_rows, group_rows as above.  0 <= K <= Q8_MAX_K, any alignment of the codes.
+ *   belong to an expert; out_amax is an output: it may not be an input's memory, next_scale's neither).  x_count, x_rows, group_rows as above.  0 <= K <= Q8_MAX_K, any alignment of the codes.
  */
 q8_status q8_linear_grouped(const int8_t* xq, int64_t x_count, const int32_t* x_rows, const int8_t* wq, const float* bias, const float* sx,
                             const float* sw, const int32_t* group_rows, int n_experts, int64_t M, int64_t N, int64_t K, void* y,
@@ -463,8 +464,8 @@ q8_status q8_linear_grouped(const int8_t* xq, int64_t x_count, const int32_t* x_
  * The router of a mixture of experts: each token's k experts of largest logit, and its rows in the experts' order.
  *   logits fp32[T, n_experts]; 1 <= n_experts <= Q8_ROUTE_MAX_EXPERTS, 1 <= k <= min(n_experts, Q8_ROUTE_MAX_K), T * k < 2^31.
  *   experts int32[T,k]: by falling logit, ties by rising index.  -inf (an expert that is masked out) comes last, NaN counts as -inf.
- *   gates fp32[T,k]: softmax over the k chosen logits; 0 for a logit of -inf, so all 0 for a token that has no other.  Several of +inf
- *   share the gate.
+ *   gates fp32[T,k]: softmax over the k chosen logits; 0 for a logit of -inf, so all 0 for a token that has no other.  +inf counts as the
+ *   largest finite number: several of them share the gate.
  *   group_rows int32[n_experts]: (token, choice) pairs of each expert.
  *   rows int32[T*k]: the tokens of the pairs sorted by expert, within an expert by token: the x_rows of the grouped products.
  *   slots int32[T,k]: where each pair went: rows[slots[t,j]] = t.

@@ -41,9 +41,10 @@ static bool tile_eligible(const Product& p, int64_t rows)
 //     walk a larger tile cannot hide (64 x 4096 -> 1024 4.7 and 7.6; int8, 275 rows of 16 experts, 4096 -> 512 9.5 and 19.7; but 754 rows of 8 experts, 2048 ->
 //     1024, about 900, 14.6 and 9.1).
 //   5 (256x256) for long rows whose tiles leave less than a quarter of a round of the 256 units idle: it moves the fewest operand bytes, but a unit holds one at
-//     a time and waits for the last round (4096 -> 1024 to bf16: 14336 rows, 224 tiles, 36.2 and 128x128 38.9; 24576 rows, 384, 66.7 and 57.6).  Rows have to be
-//     4 KiB for several rounds (8192 x 8192 -> 4096 134 and 141; 8192 x 4096 -> 4096 77 and 74), 8 KiB for int8 (4096 x 16384 -> 4096 223 and 255; 14336 x 4096 ->
-//     1024 64.0 and 64.3) and for fp32 outputs, whose stores nothing covers (4096 x 16384 -> 4096 135 and 141; 4096 x 4096 -> 4096 51 and 42).
+//     a time and waits for the last round (4096 -> 1024 to bf16: 14336 rows, 224 tiles, 36.8 and 128x128 38.2; 24576 rows, 384, 66.9 and 56.4, of 16 experts 68.2 and
+//     63.3; codes of normal numbers, on those of a layer behind a GELU within 2 % of that).  Rows have to be 4 KiB for several rounds (8192 x 8192 -> 4096 133 and 139;
+//     8192 x 4096 -> 4096 78 and 73), 8 KiB for int8 (4096 x 16384 -> 4096 223 and 255; 14336 x 4096 -> 1024 64.0 and 64.3) and for fp32 outputs, whose stores
+//     nothing covers (4096 x 16384 -> 4096 135 and 141; 4096 x 4096 -> 4096 45 and 40).
 //   4 (128x128) from two tiles a unit on (8192 x 2048 -> 4096 to bf16 40.8, 64x128 51.9; 12288 x 1024 -> 4096 37 and 44.5), three where groups are smaller than a
 //     tile (57 rows each of 128, int8, 768 -> 1024 23.3 and 25.4; but 29 rows each 17.9 and 16.9), of long rows from one and a half.
 //   3 (64x128) against 2 (64x64): from two tiles a unit on (8192 rows of 16 experts, 512 -> 4096 24.5 and 32.4), unless rows are short and groups small (4809 rows

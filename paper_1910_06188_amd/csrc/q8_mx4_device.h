@@ -27,8 +27,8 @@ __device__ __forceinline__ unsigned mx4_scale_byte(unsigned amax_bits)
 __device__ __forceinline__ float mx4_scale(unsigned byte) { return __uint_as_float(byte ? byte << 23 : 0x00400000u); }
 
 // Eight elements of one block to eight codes, the first in the low half of the low byte.  v_cvt_scalef32_pk_fp4_f32 divides by
-// the power of two, rounds to the nearest code with ties to even, keeps the sign and takes magnitudes above 6 to 6 (checked on
-// all quotients of 13 bits below 8 at 253 scales, and at scale 2^-127).
+// the power of two, rounds to the nearest code with ties to even, keeps the sign and takes magnitudes above 6 to 6 (tested on
+// all quotients of 12 bits below 8, both signs, in blocks of ten magnitudes from subnormal ones to 2^126).
 __device__ __forceinline__ unsigned mx4_codes8(const float* v, unsigned byte)
 {
     const float s = mx4_scale(byte);

@@ -5,8 +5,9 @@
 //   workgroup = KW waves, one tile of up to 32 rows and 32 columns
 //   wave w    = the 128-byte units w, w + KW, ... of the reduction: four 1 KiB loads of whole lines of w, through LDS of its own
 //
-// As two launches and as one: 1 x 1024 -> 4096 6.2 and 3.6 us, 8 x 1024 -> 4096 6.4 and 4.2, 256 x 512 -> 512 6.6 and 5.1, 128 x 768 -> 768 6.8 and 6.2; from
-// 32 rows of 1024 on two are as fast (6.5 and 7.0), and many tiles slower as one (512 x 1024 -> 1024 7.8 and 10.5).
+// As two launches and as one, us a call in a loop on one set of tensors: 1 x 1024 -> 4096 6.4 and 3.4, 8 x 1024 -> 4096 6.3 and 4.0, 256 x 512 -> 512 6.6 and 5.0,
+// 128 x 768 -> 768 6.6 and 6.0; from 32 rows of 1024 on two are as fast (6.5 and 7.0), and many tiles slower as one (512 x 1024 -> 1024 7.8 and 10.5).  With the
+// tensors of several layers in turn 1 x 1024 -> 4096 takes 4.6 to 4.8 a call; the kernel itself 3.8.
 #include "q8_grouped_device.h"
 #include "q8_load16.h"
 
