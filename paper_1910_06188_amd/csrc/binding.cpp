@@ -33,7 +33,10 @@ T argument(PyObject* o)
             return nullptr;
         }
         const at::Tensor& t = THPVariable_Unpack(o);
-        if (!t.is_cuda())
+        // of floats of two bytes and one the calls would read and write as many elements of four
+        if (std::is_same_v<std::remove_cv_t<std::remove_pointer_t<T>>, float> && at::isFloatingType(t.scalar_type()) && t.element_size() < 4)
+            PyErr_SetString(PyExc_TypeError, "q8 takes float32 tensors here");
+        else if (!t.is_cuda())
             PyErr_SetString(PyExc_ValueError, "q8 takes device tensors");
         else if (!t.is_contiguous())
             PyErr_SetString(PyExc_ValueError, "q8 takes contiguous tensors");

@@ -98,3 +98,16 @@ def test_the_gelu_polynomial_is_written_once():
     text = "".join(open(os.path.join(csrc, f)).read() for f in sorted(os.listdir(csrc)))
     for constant in ("3.309277963e-05f", "9.999930859e-01f"):
         assert text.count(constant) == 1
+
+
+def test_fp32_entry_points_refuse_shorter_floats():
+    """bf16 activations belong to the 4-bit entry points; those of fp32 would read twice as many bytes as such a tensor has."""
+    import torch
+    from paper_1910_06188_amd import q8
+    f, one, work, q = torch.zeros(64), torch.zeros(1), torch.zeros(q8.SCAL_WORK), torch.zeros(64, dtype=torch.int8)
+    for kind in (torch.bfloat16, torch.float16):
+        x = torch.zeros(64, dtype=kind)
+        for call in (lambda: q8.q8_absmax(x, one), lambda: q8.q8_quantize(x, one, q), lambda: q8.q8_quantize_dynamic(x, q, work), lambda: q8.q8_fake_quantize(x, one, f),
+                     lambda: q8.q8_fake_quantize_ema(x, 0.9, f, work, f), lambda: q8.q8_ste_backward(x, f)):
+            with pytest.raises(TypeError):
+                call()
