@@ -438,7 +438,7 @@ q8_status q8_mx4_linear_dynamic(const void* x, int x_type, const uint8_t* wq, co
  * next group_rows[1] to expert 1, ...
  *     y[r,n] = act(sum_k x[x_rows[r],k] w[e(r),n,k] + bias[e(r),n])
  *   xq, xs: codes and scales of x [x_count, K]; x_rows int32[M] the row of x that each row of y reads, or NULL: x has M rows and row r
- *   reads row r.  An index outside x counts as a row of zeros; nothing is read out of bounds.
+ *   reads row r.  An index outside x counts as a row of zeros; nothing is read out of bounds.  x_count >= 1.
  *   wq, ws: codes and scales of n_experts matrices [N,K]; bias fp32[n_experts, N] or NULL.
  *   group_rows int32[n_experts], on the device, as q8_route leaves it.  Negative numbers count as zero, and rows beyond M do not exist:
  *   whatever it holds, nothing outside y is written.  Rows of y behind the last group's stay as they are (a buffer may be larger than

@@ -355,3 +355,93 @@ def test_outputs_stored_for_the_caches_and_past_them(q8, v, M):
     finally:
         q8.set_product_variant(0)
     assert torch.equal(half, y.bfloat16())
+
+
+# ---- large tensors, and none of a reduction -------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("M", [9, 600])
+@pytest.mark.parametrize("flags", [0, 1, 3, 6])
+def test_int8_grouped_without_a_reduction(q8, variant, M, flags):
+    """K = 0: the quantized bias alone, as q8_linear has it."""
+    g = np.random.default_rng(M)
+    N, counts = 70, [M // 3, 0, M - M // 3 - 2]
+    b, sw = dev(g.standard_normal((3, N)).astype(np.float32)), dev(np.array([900, 1000, 1100], np.float32))
+    sx, ns = torch.tensor([31.7], device="cuda"), torch.tensor([40.0], device="cuda")
+    x, w = torch.empty((M, 0), dtype=torch.int8, device="cuda"), torch.empty((3, N, 0), dtype=torch.int8, device="cuda")
+    kind = torch.int8 if flags & q8.EPI_REQUANT else torch.float32
+    y, amax, want, want_amax = torch.full((M, N), 7, dtype=kind, device="cuda"), torch.zeros(1, device="cuda"), torch.full((M, N), 7, dtype=kind, device="cuda"), torch.zeros(1, device="cuda")
+    q8.q8_linear_grouped(x, w, b, sx, sw, dev(np.array(counts, np.int32)), y, out_amax=amax, next_scale=ns, flags=flags)
+    for e, (a, z) in enumerate(MX.spans(counts, M)):
+        if z > a:
+            q8.q8_linear(x[a:z], w[e], b[e], sx, sw[e: e + 1], want[a:z], out_amax=want_amax, next_scale=ns, flags=flags)
+    assert torch.equal(y, want) and torch.equal(amax, want_amax)
+
+
+@pytest.mark.parametrize("v", [0, 1, 4])
+def test_grouped_weights_beyond_32_bits(q8, v):
+    """5.4 GB of codes: rows of the first and the last experts."""
+    E, N, K, M = 80, 16384, 8192, 400
+    g = torch.Generator(device="cuda")
+    g.manual_seed(v)
+    rand = lambda *s, lo=0, hi=256: torch.randint(lo, hi, s, generator=g, device="cuda", dtype=torch.uint8)  # noqa: E731
+    xq, wq = (rand(M, K // 2), rand(K // 128, M, 4, lo=118, hi=128)), (rand(E, N, K // 2), rand(E, K // 128, N, 4, lo=118, hi=128))
+    counts = torch.zeros(E, dtype=torch.int32, device="cuda")
+    counts[0], counts[40], counts[E - 1] = 100, 130, M - 230
+    y = torch.full((M, N), float("nan"), device="cuda")
+    q8.set_product_variant(v)
+    try:
+        q8.q8_mx4_linear_grouped(*xq, *wq, None, counts, y)
+    finally:
+        q8.set_product_variant(0)
+    cols = torch.tensor([0, 1, 127, 8191, N - 2, N - 1], device="cuda")
+    xv = MX.values(host(xq[0]), host(xq[1]))
+    for e, a, z in ((0, 0, 100), (40, 100, 230), (E - 1, 230, M)):
+        wv = MX.values(host(wq[0][e][cols]), host(wq[1][e][:, cols]))
+        err = (K / 64 + 10) * 2.0 ** -23 * (np.abs(xv[a:z]) @ np.abs(wv).T)      # K / 64 instructions, eight partial sums
+        assert (np.abs(host(y[a:z][:, cols]) - xv[a:z] @ wv.T) <= err).all()
+    assert not y.isnan().any()
+
+
+@pytest.mark.parametrize("kind", [torch.float32, torch.bfloat16])
+def test_combine_of_rows_beyond_32_bits(q8, kind):
+    """4.6e9 elements of y and of out: first and last tokens."""
+    R, N, k, T = 70000, 65536, 2, 70000
+    y = torch.zeros((R, N), dtype=kind, device="cuda")
+    y[:50], y[-50:] = torch.randn(50, N, device="cuda"), torch.randn(50, N, device="cuda")
+    slots = torch.arange(T, dtype=torch.int32, device="cuda")[:, None].repeat(1, k)
+    slots[:, 1] = T - 1 - slots[:, 1]
+    gates = torch.rand(T, k, device="cuda")
+    out = torch.full((T, N), 7, dtype=kind, device="cuda")
+    q8.q8_combine(y, slots, gates, out)
+    for t in (0, 1, 49, T - 50, T - 1):
+        terms = gates[t].double()[:, None] * y[slots[t].long()].double()
+        ref, mag = terms.sum(0), terms.abs().sum(0)
+        err = k * 2.0 ** -24 * 1.001 * mag            # k fused additions, each rounded once
+        if kind is torch.bfloat16:
+            err = err + 2.0 ** -8 * (ref.abs() + err)
+        assert ((out[t].double() - ref).abs() <= err).all()
+    assert not out[60: 2000].any() and not out[T - 2000: T - 60].any()
+    del y, out
+    torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("T,E,k", [(1_500_000, 8, 2), (400_000, 200, 6)])
+def test_route_of_millions_of_tokens(q8, T, E, k):
+    """Long runs: against a stable sort of the logits and one of the choices."""
+    g = torch.Generator(device="cuda")
+    g.manual_seed(T)
+    l = (torch.randn(T, E, generator=g, device="cuda") * 8).round() / 8                # many ties
+    i32 = dict(dtype=torch.int32, device="cuda")
+    experts, rows, slots, gates = torch.empty((T, k), **i32), torch.empty(T * k, **i32), torch.empty((T, k), **i32), torch.empty((T, k), device="cuda")
+    counts, work = torch.empty(E, **i32), torch.empty(q8.ROUTE_BLOCKS * E, **i32)
+    q8.q8_route(l, experts, gates, counts, rows, slots, work)
+    top, want = (t[:, :k] for t in l.sort(dim=1, descending=True, stable=True))
+    assert torch.equal(experts, want.int())
+    flat = want.reshape(-1)
+    order = flat.argsort(stable=True)
+    assert torch.equal(counts, torch.bincount(flat, minlength=E).int()) and torch.equal(rows, (order // k).int())
+    place = torch.empty_like(order)
+    place[order] = torch.arange(T * k, device="cuda")
+    assert torch.equal(slots.view(-1), place.int())
+    # logits within 16 of each other: an argument rounded once, exp within two ulps, a sum of k and a division
+    assert ((gates.double() - torch.softmax(top.double(), 1)).abs() <= (16 * 2.0 ** -24 + 2.0 ** -21 + k * 2.0 ** -23) * torch.softmax(top.double(), 1)).all()
